@@ -420,6 +420,144 @@ int ee_vocab_signals(const float* x, const uint16_t* gain, const uint16_t* U, in
 int ee_select_tau(const float* conf, int conf_stride, const int32_t* member, int n, float target, float* tau,
                   void* scratch, void* stream);
 
+/* ---- operators that train and score a readout --------------------------
+ *
+ * A readout is fitted by distilling the full model's answers into it (Section
+ * 2; Section 4 step two) and judged by the probabilities it gives.  The calls
+ * below are that program's building blocks, on device buffers of the caller:
+ * affine maps and RMSNorm with their gradients, log probabilities of given
+ * tokens with the best alternatives, and the distillation loss with its
+ * gradient.
+ *   - Everything is enqueued on `stream` (a cudaStream_t); nothing
+ *     synchronises, allocates or is kept between calls.  Scratch contents do
+ *     not matter before a call and mean nothing after it.
+ *   - Matrices are row-major with a row stride `ld` in elements (>= the width;
+ *     any alignment of the element type; 16-byte aligned rows are fastest).
+ *     Outputs must not overlap inputs unless a call says so.
+ *   - rows may be 0: gradients summed over rows are then zero, nothing else is
+ *     written.
+ *   - Sums, norms and softmax statistics are held in 32 bits; results are
+ *     rounded once, to their type.  Results do not depend on the schedule: no
+ *     sum is made of floating-point atomics. */
+#define EE_BF16 0
+#define EE_FP16 1
+#define EE_FP32 2
+
+#define EE_ACT_NONE 0
+#define EE_ACT_RELU 1
+#define EE_ACT_SILU 2
+#define EE_ACT_GELU 3 /* u (1 + erf(u / sqrt 2)) / 2 */
+
+#define EE_MAX_TOP 128        /* entries of a list of best tokens */
+#define EE_MAX_VOCAB (1 << 23)
+#define EE_MAX_NORM 16384     /* width of ee_rms_norm */
+
+/* y = act(x W^T + b) + r for x [rows, n_in], W [n_out, n_in], b [n_out], r and
+ * y [rows, n_out].  x, W and b have type EE_BF16 or EE_FP16 (`type`); y and r
+ * that type or EE_FP32 (out_type).  b, r and preact may be NULL.  preact
+ * (fp32 [rows, n_out], contiguous) receives x W^T + b for the backward pass of
+ * an activation; 32 bits, because the slope is taken from it.  r may be y.
+ * Should one of the kernel's waits run out (about 2 s), the results it could
+ * not compute are NaN. */
+typedef struct {
+    int32_t type, out_type, activation, n_in, n_out;
+    int64_t rows;
+    const void* x;
+    int64_t ld_x;
+    const void* w;
+    int64_t ld_w;
+    const void* bias;
+    const void* residual;
+    int64_t ld_residual;
+    void* out;
+    int64_t ld_out;
+    float* preact;
+} ee_linear_args;
+/* Scratch for exactly these arguments (0 for most): 256-byte aligned. */
+int ee_linear_scratch_bytes(const ee_linear_args* args, size_t* bytes);
+int ee_linear(const ee_linear_args* args, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Gradients of ee_linear for dy [rows, n_out], each where its pointer is not
+ * NULL (the residual's is dy itself):
+ *   du = dy act'(preact);  dx = du W [rows, n_in];  dw = du^T x [n_out, n_in],
+ *   contiguous, of the operands' type or EE_FP32 (dw_type);  dbias = sum over
+ *   rows of du, fp32 [n_out].
+ * Behind an activation du is rounded to the operands' type for the two
+ * products (the tensor cores take 16-bit operands); dbias sums it unrounded.
+ * x is needed for dw, w for dx, preact with an activation. */
+typedef struct {
+    int32_t type, activation, n_in, n_out;
+    int64_t rows;
+    const void* dy;
+    int64_t ld_dy;
+    const void* x;
+    int64_t ld_x;
+    const void* w;
+    int64_t ld_w;
+    const float* preact;
+    void* dx;
+    int64_t ld_dx;
+    void* dw;
+    int32_t dw_type, reserved;
+    float* dbias;
+} ee_linear_grad_args;
+int ee_linear_backward_scratch_bytes(const ee_linear_grad_args* args, size_t* bytes);
+int ee_linear_backward(const ee_linear_grad_args* args, void* scratch, size_t scratch_bytes, void* stream);
+
+/* y = x r g with r = 1 / sqrt(mean x^2 + eps) per row of d <= EE_MAX_NORM
+ * elements; gain [d].  Any mix of element types.  rstd (fp32 [rows], may be
+ * NULL) receives r for the backward pass.  y may be x (same type and stride). */
+int ee_rms_norm(const void* x, int x_type, int64_t rows, int d, int64_t ld_x, const void* gain, int gain_type, float eps,
+                void* y, int y_type, int64_t ld_y, float* rstd, void* stream);
+/* dx = r (g dy - x r^2 mean(g dy x)), of x's type, and dgain = sum over rows of
+ * dy x r, fp32 [d]; either may be NULL.  dx may be dy (same type and stride).
+ * scratch (16-byte aligned) is needed for dgain. */
+int ee_rms_norm_scratch_bytes(int64_t rows, int d, size_t* bytes);
+int ee_rms_norm_backward(const void* dy, int dy_type, int64_t ld_dy, const void* x, int x_type, int64_t rows, int d,
+                         int64_t ld_x, const void* gain, int gain_type, const float* rstd, void* dx, int64_t ld_dx,
+                         float* dgain, void* scratch, size_t scratch_bytes, void* stream);
+
+/* Per row of logits z [rows, vocab], with p = softmax(z / temperature):
+ *   logprob      fp32 [rows]: log p of ids[row]; 0 where ids[row] < 0 (no token
+ *                to score), NaN where ids[row] >= vocab; may be NULL (and ids)
+ *   entropy      fp32 [rows]: -sum p log p; may be NULL
+ *   lse          fp32 [rows]: log sum exp(z / temperature); may be NULL
+ *   top_logprob, top_id  [rows, k]: the k best tokens and their log p, best
+ *                first, equal logits by the lower index; k in 0..EE_MAX_TOP
+ * Logits of -inf have probability 0.  A row without a finite logit has entropy
+ * 0, lse and every log p -inf.  A row holding NaN or +inf gives NaN (its best
+ * tokens are still in order, NaN above +inf). */
+int ee_token_logprobs(const void* logits, int type, int64_t rows, int vocab, int64_t ld, const int32_t* ids, int k,
+                      float temperature, float* logprob, float* entropy, float* lse, float* top_logprob,
+                      int32_t* top_id, void* stream);
+
+/* Distillation of a teacher's best tokens into rows of student logits z [rows,
+ * vocab], p = softmax(z / T).  ids and teacher [rows, k] (row strides ld_ids,
+ * ld_teacher; 1 <= k <= EE_MAX_TOP): tokens and the teacher's values l for
+ * them.  An entry with its id outside [0, vocab) or its value -inf is absent.
+ * An id listed twice counts as two entries.
+ *   tail = 0: q = softmax(l) over the list (logits / T, or log probabilities)
+ *   tail = 1: q = exp(l), l being log probabilities at temperature T
+ *             (ee_token_logprobs gives them); what is left, q0 = max(0, 1 -
+ *             sum q), is compared with the student's mass p0 outside the list
+ *   loss [rows] = T^2 [ sum q (log q - log p) + q0 (log q0 - log p0) ]
+ *   grad [rows, vocab] (of the logits' type; may be NULL) = weight[row] *
+ *             d loss / d z; weight NULL: 1.  A row of weight 0 has gradient 0
+ *             whatever its logits hold.  grad may be logits (same stride).
+ *   stats     fp32 [rows, 4], 16-byte aligned: for ee_distill_topk_backward;
+ *             may be NULL
+ * An empty list gives loss 0 and gradient 0.  A row without a finite logit has
+ * loss +inf (0 for an empty list) and gradient 0. */
+int ee_distill_topk(const void* logits, int type, int64_t rows, int vocab, int64_t ld, const int32_t* ids,
+                    int64_t ld_ids, const float* teacher, int64_t ld_teacher, int k, float temperature, int tail,
+                    float* loss, float* stats, const float* weight, void* grad, int64_t ld_grad, void* stream);
+/* The gradient alone: grad = dloss[row] * d loss / d z, from the same arguments
+ * and the forward call's stats.  grad may be logits (same stride). */
+int ee_distill_topk_backward(const float* dloss, const void* logits, int type, int64_t rows, int vocab, int64_t ld,
+                             const int32_t* ids, int64_t ld_ids, const float* teacher, int64_t ld_teacher, int k,
+                             float temperature, int tail, const float* stats, void* grad, int64_t ld_grad,
+                             void* stream);
+
 #ifdef __cplusplus
 }
 #endif

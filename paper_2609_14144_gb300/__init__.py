@@ -17,7 +17,23 @@ from ._lib import (CONF_MARGIN, CONF_NEGENT, CONF_PMAX, DEVICE, FORCE_FULL, FREE
                    EEError, FORCE_EXIT_AT, check)
 
 __all__ = ["Engine", "EEError", "FREE", "FORCE_FULL", "FORCE_EXIT_AT", "HOST", "DEVICE", "attention_decode",
-           "vocab_confidence", "vocab_signals", "select_tau", "library_path"]
+           "vocab_confidence", "vocab_signals", "select_tau", "library_path", "linear", "linear_backward", "rms_norm",
+           "rms_norm_backward", "token_logprobs", "distill_topk", "distill_topk_step", "distill_topk_backward"]
+
+_OPERATORS = ("linear", "linear_backward", "rms_norm", "rms_norm_backward", "token_logprobs", "distill_topk",
+              "distill_topk_step", "distill_topk_backward")
+
+
+def __getattr__(name: str):
+    """The operators on torch tensors, imported when first used: the package
+    itself loads without torch."""
+    if name in _OPERATORS:
+        from . import operators
+
+        for op in _OPERATORS:
+            globals()[op] = getattr(operators, op)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def library_path() -> str:

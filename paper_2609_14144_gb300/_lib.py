@@ -14,6 +14,7 @@ OPT_GRAPHS, OPT_PDL, OPT_DEBUG_LOGITS, OPT_PERSISTENT, OPT_CONFIDENCE, OPT_NUCLE
 OPT_ROWS = 8
 OPT_WAIT_LIMIT = 9
 OPT_LAZY_FILL = 11
+BF16, FP16, FP32 = 0, 1, 2  # element types of the operators
 CONF_PMAX, CONF_MARGIN, CONF_NEGENT = 0, 1, 2
 DBG_HIDDEN_READOUT, DBG_READOUT_Y, DBG_HIDDEN_FINAL, DBG_READOUT_LOGITS, DBG_FINAL_LOGITS, DBG_KV, DBG_KV_SRC = \
     1, 2, 3, 4, 5, 6, 7
@@ -23,7 +24,10 @@ SYMBOLS = ("ee_workspace_bytes", "ee_create", "ee_destroy", "ee_last_error", "ee
            "ee_set_page_table", "ee_reset", "ee_prefill", "ee_decode_step", "ee_decode_n", "ee_sync",
            "ee_get_stats", "ee_position", "ee_set_option", "ee_debug_read", "ee_attention_scratch_bytes",
            "ee_attention_decode", "ee_vocab_scratch_bytes", "ee_vocab_confidence", "ee_vocab_signals", "ee_profile_kernels",
-           "ee_attention_decode_static", "ee_calibrate", "ee_select_tau", "ee_repass", "ee_flush_fills")
+           "ee_attention_decode_static", "ee_calibrate", "ee_select_tau", "ee_repass", "ee_flush_fills",
+           "ee_linear_scratch_bytes", "ee_linear", "ee_linear_backward_scratch_bytes", "ee_linear_backward",
+           "ee_rms_norm", "ee_rms_norm_scratch_bytes", "ee_rms_norm_backward", "ee_token_logprobs", "ee_distill_topk",
+           "ee_distill_topk_backward")
 KERNELS = ("qkv", "attention", "oproj", "gateup", "down", "readout", "vocab", "kvfill", "layers")
 
 
@@ -68,6 +72,21 @@ class StepResult(ctypes.Structure):
 class Stats(ctypes.Structure):
     _fields_ = [("steps", ctypes.c_int64), ("full_steps", ctypes.c_int64),
                 ("exits", ctypes.c_int64 * MAX_READOUTS)]
+
+
+class LinearArgs(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("out_type", ctypes.c_int32), ("activation", ctypes.c_int32),
+                ("n_in", ctypes.c_int32), ("n_out", ctypes.c_int32), ("rows", ctypes.c_int64), ("x", _P),
+                ("ld_x", ctypes.c_int64), ("w", _P), ("ld_w", ctypes.c_int64), ("bias", _P), ("residual", _P),
+                ("ld_residual", ctypes.c_int64), ("out", _P), ("ld_out", ctypes.c_int64), ("preact", _P)]
+
+
+class LinearGradArgs(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("activation", ctypes.c_int32), ("n_in", ctypes.c_int32),
+                ("n_out", ctypes.c_int32), ("rows", ctypes.c_int64), ("dy", _P), ("ld_dy", ctypes.c_int64), ("x", _P),
+                ("ld_x", ctypes.c_int64), ("w", _P), ("ld_w", ctypes.c_int64), ("preact", _P), ("dx", _P),
+                ("ld_dx", ctypes.c_int64), ("dw", _P), ("dw_type", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("dbias", _P)]
 
 
 _lib = None
@@ -122,6 +141,16 @@ def load(allow_build: bool = False):
     lib.ee_repass.argtypes = [_P, i32, i32, ctypes.POINTER(i32)]
     lib.ee_calibrate.argtypes = [_P, _P, ctypes.c_int, ctypes.c_float, _P, _P, _P, ctypes.c_int]
     lib.ee_select_tau.argtypes = [_P, ctypes.c_int, _P, ctypes.c_int, ctypes.c_float, _P, _P, _P]
+    i64, ci, cf = ctypes.c_int64, ctypes.c_int, ctypes.c_float
+    for op, args in (("ee_linear", LinearArgs), ("ee_linear_backward", LinearGradArgs)):
+        getattr(lib, op + "_scratch_bytes").argtypes = [ctypes.POINTER(args), ctypes.POINTER(sz)]
+        getattr(lib, op).argtypes = [ctypes.POINTER(args), _P, sz, _P]
+    lib.ee_rms_norm.argtypes = [_P, ci, i64, ci, i64, _P, ci, cf, _P, ci, i64, _P, _P]
+    lib.ee_rms_norm_scratch_bytes.argtypes = [i64, ci, ctypes.POINTER(sz)]
+    lib.ee_rms_norm_backward.argtypes = [_P, ci, i64, _P, ci, i64, ci, i64, _P, ci, _P, _P, i64, _P, _P, sz, _P]
+    lib.ee_token_logprobs.argtypes = [_P, ci, i64, ci, i64, _P, ci, cf, _P, _P, _P, _P, _P, _P]
+    lib.ee_distill_topk.argtypes = [_P, ci, i64, ci, i64, _P, i64, _P, i64, ci, cf, ci, _P, _P, _P, _P, i64, _P]
+    lib.ee_distill_topk_backward.argtypes = [_P, _P, ci, i64, ci, i64, _P, i64, _P, i64, ci, cf, ci, _P, _P, i64, _P]
     for name in SYMBOLS:
         f = getattr(lib, name)
         if name != "ee_last_error":

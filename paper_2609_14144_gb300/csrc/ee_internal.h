@@ -340,4 +340,8 @@ constexpr int kGemvMaxSmem = 227 * 1024;  // dynamic shared memory a GEMV CTA ma
 inline int64_t tile_count(int64_t rows) { return (rows + kTileRows - 1) / kTileRows; }
 inline int64_t tiled_elems(int64_t rows, int64_t K) { return tile_count(rows) * kTileRows * K; }
 
+// cuTensorMapEncodeTiled of the loaded driver (a PFN_cuTensorMapEncodeTiled_v12000),
+// or null.
+void* tensor_map_encoder();
+
 }  // namespace ee

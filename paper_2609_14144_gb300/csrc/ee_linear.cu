@@ -1,0 +1,844 @@
+// Affine maps over rows with everything that follows in the product's epilogue,
+// and their gradients (ee_linear, ee_linear_backward):
+//   u = x W^T + b,  y = act(u) + r
+//   du = dy act'(u),  dx = du W,  dW = du^T x,  db = sum over rows of du
+// Operands are bf16 or fp16, sums are held in 32 bits.
+//
+// Up to 8 rows the product is bound by reading W once: k_linear_few streams it
+// through warps, a warp per group of outputs.  More rows go to the tcgen05
+// tensor cores (k_gemm): D[M][N] = sum_k A[m][k] B[n][k] for 128 x BN tiles.
+// Each operand may be stored with k contiguous (rows of x, W, dy) or with its
+// own index contiguous (W as dx's operand, dy and x as dW's): TMA boxes of 128
+// swizzled bytes serve both, the shared-memory descriptor and the instruction's
+// transpose bits tell them apart, so nothing is transposed in memory.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "ee_internal.h"
+#include "ee_umma.cuh"
+
+namespace ee {
+namespace {
+
+constexpr unsigned kFull = 0xffffffffu;
+constexpr int kFewRows = 8;
+
+// ---------------------------------------------------------------- 16-bit values
+__device__ __forceinline__ float2 unpack2(uint32_t w, int type) {
+    if (type == EE_BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+__device__ __forceinline__ float get16(uint16_t h, int type) {
+    return type == EE_BF16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
+}
+__device__ __forceinline__ uint16_t put16(float f, int type) {
+    return type == EE_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(f)) : __half_as_ushort(__float2half_rn(f));
+}
+// Eight elements at p, n of them there (16-byte access where `vec`).
+__device__ __forceinline__ void load8(const void* p, int type, int n, bool vec, float (&x)[8]) {
+    if (vec && n >= 8) {
+        const uint4 a = *(const uint4*)p;
+        if (type == EE_FP32) {
+            const uint4 b = ((const uint4*)p)[1];
+            x[0] = __uint_as_float(a.x), x[1] = __uint_as_float(a.y), x[2] = __uint_as_float(a.z);
+            x[3] = __uint_as_float(a.w), x[4] = __uint_as_float(b.x), x[5] = __uint_as_float(b.y);
+            x[6] = __uint_as_float(b.z), x[7] = __uint_as_float(b.w);
+        } else {
+            const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = unpack2(w[i], type);
+                x[2 * i] = f.x, x[2 * i + 1] = f.y;
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        x[i] = i >= n ? 0.f : type == EE_FP32 ? ((const float*)p)[i] : get16(((const uint16_t*)p)[i], type);
+}
+__device__ __forceinline__ void store8(void* p, int type, int n, bool vec, const float (&x)[8]) {
+    if (type == EE_FP32) {
+        if (vec && n >= 8) {
+            ((float4*)p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+            ((float4*)p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) ((float*)p)[i] = x[i];
+        return;
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = put16(x[2 * i], type) | (uint32_t)put16(x[2 * i + 1], type) << 16;
+    if (vec && n >= 8) {
+        *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < n) ((uint16_t*)p)[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+}
+__host__ __device__ __forceinline__ int bytes_of(int type) { return type == EE_FP32 ? 4 : 2; }
+
+// ---------------------------------------------------------------- activations
+__device__ __forceinline__ float act_value(float u, int act) {
+    if (act == EE_ACT_RELU) return u > 0.f || u != u ? u : 0.f;
+    if (act == EE_ACT_SILU) return u / (1.f + expf(-u));
+    if (act == EE_ACT_GELU) return 0.5f * u * (1.f + erff(u * 0.70710678f));
+    return u;
+}
+__device__ __forceinline__ float act_slope(float u, int act) {
+    if (act == EE_ACT_RELU) return u > 0.f ? 1.f : 0.f;
+    if (act == EE_ACT_SILU) {
+        const float g = 1.f / (1.f + expf(-u));
+        return g * fmaf(u, 1.f - g, 1.f);
+    }
+    if (act == EE_ACT_GELU) return 0.5f * (1.f + erff(u * 0.70710678f)) + u * expf(-0.5f * u * u) * 0.39894228f;
+    return 1.f;
+}
+
+// What follows a sum: bias, the value kept for the backward pass, activation,
+// residual, and the one rounding to the result's type.
+struct Epilogue {
+    const void* bias;
+    const void* res;
+    void* out;
+    float* preact;
+    int64_t ld_res, ld_out, ld_pre;
+    int type, out_type, act;
+    bool vec_bias, vec_res, vec_out, vec_pre;  // 16-byte access at multiples of 8 columns
+};
+__device__ __forceinline__ void emit8(const Epilogue& e, int64_t row, int64_t col, int n, float (&v)[8]) {
+    if (e.bias) {
+        float b[8];
+        load8((const char*)e.bias + col * 2, e.type, n, e.vec_bias, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += b[i];
+    }
+    if (e.preact) store8(e.preact + row * e.ld_pre + col, EE_FP32, n, e.vec_pre, v);
+    if (e.act != EE_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = act_value(v[i], e.act);
+    }
+    if (e.res) {
+        float r[8];
+        load8((const char*)e.res + (row * e.ld_res + col) * bytes_of(e.out_type), e.out_type, n, e.vec_res, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += r[i];
+    }
+    store8((char*)e.out + (row * e.ld_out + col) * bytes_of(e.out_type), e.out_type, n, e.vec_out, v);
+}
+
+// ---------------------------------------------------------------- few rows
+// R rows (rows past `rows` repeat the last one and are not written), WN outputs
+// per warp; a lane takes 8 columns of every 256.
+template <int R, int WN, bool VEC>
+__global__ void __launch_bounds__(128) k_linear_few(const uint16_t* __restrict__ x, int64_t ld_x, int rows,
+                                                    const uint16_t* __restrict__ w, int64_t ld_w, int n_in, int n_out,
+                                                    Epilogue e) {
+    const int lane = threadIdx.x & 31;
+    const int o0 = (blockIdx.x * 4 + (threadIdx.x >> 5)) * WN;
+    if (o0 >= n_out) return;
+    float acc[WN][R];
+#pragma unroll
+    for (int i = 0; i < WN; ++i)
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[i][r] = 0.f;
+#pragma unroll 2
+    for (int c = lane * 8; c < n_in; c += 256) {
+        float wv[WN][8];
+#pragma unroll
+        for (int i = 0; i < WN; ++i) {
+            const int o = o0 + i < n_out ? o0 + i : n_out - 1;
+            load8(w + o * ld_w + c, e.type, n_in - c, VEC, wv[i]);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float xv[8];
+            load8(x + (r < rows ? r : rows - 1) * ld_x + c, e.type, n_in - c, VEC, xv);
+#pragma unroll
+            for (int i = 0; i < WN; ++i)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) acc[i][r] = fmaf(wv[i][k], xv[k], acc[i][r]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < WN; ++i)
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int o = 16; o; o >>= 1) acc[i][r] += __shfl_xor_sync(kFull, acc[i][r], o);
+    // lane r writes row r
+#pragma unroll
+    for (int i = 0; i < WN; ++i) {
+        float v[8] = {};
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (lane == r) v[0] = acc[i][r];
+        if (lane < rows && lane < R && o0 + i < n_out) emit8(e, lane, o0 + i, 1, v);
+    }
+}
+
+// ---------------------------------------------------------------- tensor cores
+constexpr int kTM = 128, kTK = 64;        // tile rows; k per stage: 128 bytes
+constexpr int kChain = 8;                 // stages the tensor core adds up by itself
+constexpr int kEpiWarps = 8;
+constexpr int kGemmThreads = 32 * (4 + kEpiWarps);
+constexpr int kABytes = kTM * kTK * 2;
+
+template <int BN>
+struct GShape {
+    static constexpr int b_bytes = BN * kTK * 2, stage = kABytes + b_bytes;
+    static constexpr int ST = 196608 / stage;  // 4, 6 or 8 stages in 192 KB
+    static constexpr int tmem = 2 * BN;        // two accumulators
+    static constexpr size_t smem = (size_t)ST * stage + kEpiWarps * 4096 + 1024 + 512;
+};
+
+// Shared-memory descriptor, 128-byte swizzle.  k contiguous: rows of 128 bytes,
+// groups of 8 of them `sbo` = 1024 bytes apart.  Own index contiguous: 64 of it
+// make such a row, one row per k, groups of 8 k 1024 bytes apart (sbo) and the
+// next 64 of the index a whole block of 64 k further (lbo).
+__device__ __forceinline__ uint64_t sw128_desc(uint32_t saddr, bool mn) {
+    uint64_t d = (uint64_t)((saddr >> 4) & 0x3fffu);
+    d |= (uint64_t)((mn ? kTK * 128 : 16) >> 4) << 16;
+    d |= (uint64_t)(1024 >> 4) << 32;
+    d |= (uint64_t)1 << 46;
+    d |= (uint64_t)2 << 61;
+    return d;
+}
+
+__device__ __forceinline__ void tma_2d(void* dst, const CUtensorMap* map, int c0, int c1, uint64_t* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+            u_saddr(dst)),
+        "l"(map), "r"(c0), "r"(c1), "r"(u_saddr(bar))
+        : "memory");
+}
+__device__ __forceinline__ void expect_tx(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(u_saddr(bar)), "r"(bytes) : "memory");
+}
+
+struct GemmArgs {
+    int M, N, nk;        // nk: stages over the whole k range
+    int mt, nt, S;       // tiles, k splits
+    int bf16;
+    float* part;         // S > 1: partial sums [S][M][ldp]
+    int64_t ldp;
+    Epilogue e;
+};
+
+// A persistent CTA per SM.  Warp 0 feeds the ring of stages by TMA, warp 1
+// issues the MMAs, warps 4 to 11 read the accumulators back.  A work item is
+// one tile over one k split; its stages are issued in chains of 8 into two
+// tensor-memory accumulators in turn, and each chain is added to the item's
+// sums in registers, rounding to nearest: the tensor core truncates as it adds,
+// so a long range in one chain would drift (the error grows with its steps).
+// The next chain, or the next item's first, runs while one is read back.
+// A wait that runs out (about 2 s) ends the CTA's loops; its remaining items
+// are written as NaN.
+template <int BN, bool A_MN, bool B_MN>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    k_gemm(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, GemmArgs g) {
+    using G = GShape<BN>;
+    extern __shared__ __align__(1024) uint8_t g_smem_raw[];
+    uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(g_smem_raw) + 1023) & ~(uintptr_t)1023);
+    float* stage_out = reinterpret_cast<float*>(sm + G::ST * G::stage);
+    uint64_t* full = reinterpret_cast<uint64_t*>(sm + G::ST * G::stage + kEpiWarps * 4096);
+    uint64_t* empty = full + G::ST;
+    uint64_t* acc_full = empty + G::ST;
+    uint64_t* acc_empty = acc_full + 2;
+    uint64_t* done = acc_empty + 2;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+    volatile int* stall = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < G::ST; ++i) {
+            u_mb_init(&full[i], 1);
+            u_mb_init(&empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            u_mb_init(&acc_full[i], 1);
+            u_mb_init(&acc_empty[i], kEpiWarps);
+        }
+        u_mb_init(done, 1);
+        *stall = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (w == 2) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(u_saddr(tmem_slot)),
+                     "r"(G::tmem)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    u_fence_before();
+    __syncthreads();
+    u_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const int tiles = g.mt * g.nt, items = tiles * g.S;
+
+    if (w < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (w == 0 && lane == 0) {  // producer
+            int64_t i = 0;
+            bool ok = true;
+            for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+                const int tile = it % tiles, s = it / tiles, m0 = tile % g.mt * kTM, n0 = tile / g.mt * BN;
+                const int k0 = (int)((int64_t)g.nk * s / g.S), k1 = (int)((int64_t)g.nk * (s + 1) / g.S);
+                for (int k = k0; k < k1; ++k, ++i) {
+                    const int st = (int)(i % G::ST);
+                    if (i >= G::ST && !u_mb_wait(&empty[st], (int)(i / G::ST - 1) & 1, stall)) {
+                        *stall = kErrStall;
+                        ok = false;
+                        break;
+                    }
+                    uint8_t* a = sm + st * G::stage;
+                    uint8_t* b = a + kABytes;
+                    expect_tx(&full[st], G::stage);
+                    if (A_MN) {
+#pragma unroll
+                        for (int j = 0; j < kTM / 64; ++j) tma_2d(a + j * kTK * 128, &ma, m0 + 64 * j, k * kTK, &full[st]);
+                    } else
+                        tma_2d(a, &ma, k * kTK, m0, &full[st]);
+                    if (B_MN) {
+#pragma unroll
+                        for (int j = 0; j < BN / 64; ++j) tma_2d(b + j * kTK * 128, &mb, n0 + 64 * j, k * kTK, &full[st]);
+                    } else
+                        tma_2d(b, &mb, k * kTK, n0, &full[st]);
+                }
+            }
+            // every issued copy lands before the CTA may leave
+            for (int64_t j = i > G::ST ? i - G::ST : 0; j < i; ++j)
+                u_mb_wait(&full[j % G::ST], (int)(j / G::ST) & 1, nullptr);
+        } else if (w == 1 && lane == 0) {  // MMA issuer
+            const uint32_t idesc = (1u << 4) | (g.bf16 ? 1u << 7 | 1u << 10 : 0u) | (A_MN ? 1u << 15 : 0u) |
+                                   (B_MN ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) | (8u << 24);
+            const uint64_t da0 = sw128_desc(u_saddr(sm), A_MN), db0 = sw128_desc(u_saddr(sm) + kABytes, B_MN);
+            constexpr uint32_t a_step = (A_MN ? 16 * 128 : 32) >> 4, b_step = (B_MN ? 16 * 128 : 32) >> 4;
+            int64_t i = 0;
+            unsigned u = 0;
+            bool ok = true;
+            for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+                const int s = it / tiles;
+                const int ks = (int)((int64_t)g.nk * (s + 1) / g.S) - (int)((int64_t)g.nk * s / g.S);
+                for (int c0 = 0; c0 < ks && ok; c0 += kChain, ++u) {
+                    if (u >= 2 && !u_mb_wait(&acc_empty[u & 1], ((u >> 1) - 1) & 1, stall)) {
+                        *stall = kErrStall;
+                        ok = false;
+                        break;
+                    }
+                    u_fence_after();
+                    const int c1 = c0 + kChain < ks ? c0 + kChain : ks;
+                    for (int k = c0; k < c1; ++k, ++i) {
+                        const int st = (int)(i % G::ST);
+                        if (!u_mb_wait(&full[st], (int)(i / G::ST) & 1, stall)) {
+                            *stall = kErrStall;
+                            ok = false;
+                            break;
+                        }
+                        u_fence_after();
+                        const uint32_t at = (uint32_t)(st * G::stage) >> 4;
+#pragma unroll
+                        for (int kk = 0; kk < kTK / 16; ++kk)
+                            u_mma(tmem + (u & 1) * BN, da0 + at + kk * a_step, db0 + at + kk * b_step, idesc,
+                                  k > c0 || kk > 0);
+                        u_commit(&empty[st]);
+                    }
+                    if (ok) u_commit(&acc_full[u & 1]);
+                }
+            }
+            u_commit(done);  // after every MMA this thread issued
+            u_mb_wait(done, 0, nullptr);
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        const int q = w & 3, h = (w - 4) >> 2;
+        constexpr int HC = BN / 2;  // columns of a warp
+        float* so = stage_out + (w - 4) * 1024;
+        const uint32_t t0 = tmem + ((uint32_t)(32 * q) << 16) + h * HC;
+        unsigned u = 0;
+        bool ok = true;
+        for (int it = blockIdx.x; it < items; it += gridDim.x) {
+            const int tile = it % tiles, s = it / tiles, m0 = tile % g.mt * kTM + 32 * q, n0 = tile / g.mt * BN + h * HC;
+            const int ks = (int)((int64_t)g.nk * (s + 1) / g.S) - (int)((int64_t)g.nk * s / g.S);
+            float acc[HC];
+#pragma unroll
+            for (int i = 0; i < HC; ++i) acc[i] = 0.f;
+            for (int c0 = 0; c0 < ks; c0 += kChain, ++u) {
+                if (ok && !u_mb_wait(&acc_full[u & 1], (u >> 1) & 1, stall)) {
+                    *stall = kErrStall;
+                    ok = false;
+                }
+                ok = __all_sync(kFull, ok);  // the loads below are warp-wide
+                if (!ok) break;
+                u_fence_after();
+#pragma unroll
+                for (int c = 0; c < HC; c += 32) {
+                    uint32_t v0[16], v1[16];
+                    u_ld16(t0 + (u & 1) * BN + c, v0);
+                    u_ld16(t0 + (u & 1) * BN + c + 16, v1);
+                    u_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        acc[c + i] += __uint_as_float(v0[i]);
+                        acc[c + 16 + i] += __uint_as_float(v1[i]);
+                    }
+                }
+                u_fence_before();
+                __syncwarp();
+                if (lane == 0) u_mb_arrive(&acc_empty[u & 1]);
+            }
+            if (!ok) {
+#pragma unroll
+                for (int i = 0; i < HC; ++i) acc[i] = __int_as_float(0x7fffffff);
+            }
+            if (m0 >= g.M) continue;
+            // 32 x 32 blocks through shared memory, so that four lanes write 32
+            // neighbouring columns of a row: 16-byte pieces, swizzled by the row
+#pragma unroll
+            for (int c = 0; c < HC; c += 32) {
+                if (n0 + c >= g.N) break;
+                float4* s4 = reinterpret_cast<float4*>(so);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    s4[lane * 8 + (j ^ (lane & 7))] =
+                        make_float4(acc[c + 4 * j], acc[c + 4 * j + 1], acc[c + 4 * j + 2], acc[c + 4 * j + 3]);
+                __syncwarp();
+                const int col = n0 + c + 8 * (lane & 3);
+#pragma unroll 1
+                for (int i = 0; i < 4; ++i) {
+                    const int lr = 8 * i + (lane >> 2), row = m0 + lr, ch = 2 * (lane & 3);
+                    const float4 a = s4[lr * 8 + (ch ^ (lr & 7))], b = s4[lr * 8 + ((ch + 1) ^ (lr & 7))];
+                    float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                    if (row < g.M && col < g.N) {
+                        if (g.S > 1)
+                            store8(g.part + ((int64_t)s * g.M + row) * g.ldp + col, EE_FP32, 8, true, v);
+                        else
+                            emit8(g.e, row, col, g.N - col, v);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    }
+    __syncwarp();
+    u_fence_before();
+    __syncthreads();
+    if (w == 2)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(G::tmem) : "memory");
+}
+
+// The splits' partial sums in split order, then the epilogue; 8 columns per
+// thread.
+__global__ void __launch_bounds__(256) k_join(GemmArgs g) {
+    const int64_t chunks = g.ldp / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= chunks * g.M) return;
+    const int64_t row = i / chunks;
+    const int col = (int)(i % chunks) * 8;
+    if (col >= g.N) return;
+    float v[8] = {};
+    for (int s = 0; s < g.S; ++s) {
+        float p[8];
+        load8(g.part + ((int64_t)s * g.M + row) * g.ldp + col, EE_FP32, 8, true, p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += p[e];
+    }
+    emit8(g.e, row, col, g.N - col, v);
+}
+
+// ---------------------------------------------------------------- around the products
+// A copy with rows on 16-byte boundaries, for operands that TMA cannot read.
+__global__ void __launch_bounds__(256) k_pack(const uint16_t* __restrict__ src, int64_t ld, int64_t rows, int cols,
+                                              uint16_t* __restrict__ dst, int64_t ldd) {
+    const int64_t per = ldd / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= rows * per) return;
+    const int64_t r = i / per;
+    const int c = (int)(i % per) * 8;
+    uint32_t w[4] = {};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (c + e < cols) w[e >> 1] |= (uint32_t)src[r * ld + c + e] << (16 * (e & 1));
+    *(uint4*)(dst + r * ldd + c) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// du = dy act'(u) rounded to the operands' type for the products (du: null to
+// skip), and this row block's column sums of the unrounded values (part: null to
+// skip).  A CTA: 256 columns, 8 threads of a warp row by row.
+__global__ void __launch_bounds__(256) k_du(const uint16_t* __restrict__ dy, int64_t ld_dy, const float* __restrict__ u,
+                                            int64_t ld_u, int64_t rows, int n_out, int type, int act, bool vec_dy,
+                                            bool vec_u, uint16_t* __restrict__ du, int64_t ld_du, float* __restrict__ part) {
+    __shared__ float sh[8][256 + 8];
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const int c = blockIdx.x * 256 + tx * 8, n = n_out - c;
+    const int64_t r0 = rows * blockIdx.y / gridDim.y, r1 = rows * (blockIdx.y + 1) / gridDim.y;
+    float sum[8] = {};
+    if (n > 0)
+#pragma unroll 4
+        for (int64_t r = r0 + ty; r < r1; r += 8) {
+            float d[8];
+            load8(dy + r * ld_dy + c, type, n, vec_dy, d);
+            if (act != EE_ACT_NONE) {
+                float v[8];
+                load8(u + r * ld_u + c, EE_FP32, n, vec_u, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d[e] *= act_slope(v[e], act);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += d[e];
+            if (du) store8(du + r * ld_du + c, type, 8, true, d);
+        }
+    if (!part) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sh[ty][tx * 8 + e] = sum[e];
+    __syncthreads();
+    float v = 0.f;
+    for (int i = 0; i < 8; ++i) v += sh[i][threadIdx.x];
+    const int col = blockIdx.x * 256 + threadIdx.x;
+    if (col < n_out) part[(int64_t)blockIdx.y * n_out + col] = v;
+}
+
+__global__ void __launch_bounds__(256) k_sum_blocks(const float* __restrict__ part, int n, int d, float* __restrict__ out) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= d) return;
+    float v = 0.f;
+    for (int i = 0; i < n; ++i) v += part[(int64_t)i * d + c];
+    out[c] = v;
+}
+
+// ---------------------------------------------------------------- host side
+int fail(int code, const char* msg) { return set_last_error(code, msg); }
+int cuda_status(cudaError_t e) { return e == cudaSuccess ? EE_OK : fail(EE_ECUDA, cudaGetErrorString(e)); }
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+bool vec_ok(const void* p, int64_t ld, int type) { return ((uintptr_t)p & 15) == 0 && ld * bytes_of(type) % 16 == 0; }
+
+// Scratch handed out piece by piece; with no memory behind it, it only counts.
+struct Carver {
+    char* base;
+    size_t at = 0;
+    void* take(size_t bytes) {
+        void* p = base ? base + at : nullptr;
+        at += align256(bytes);
+        return p;
+    }
+};
+
+// A 16-bit matrix as the products read it.
+struct Mat {
+    const uint16_t* p;
+    int64_t rows, ld;
+    int cols;
+    bool tma() const { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+};
+
+struct Ctx {
+    Carver mem;
+    bool dry;  // only count the scratch
+    int n_sm;
+    cudaStream_t s;
+    int type;
+};
+
+int n_blocks(int64_t work, int64_t per) { return (int)((work + per - 1) / per); }
+
+// m itself, or its copy with aligned rows.
+int aligned(Ctx& c, Mat* m) {
+    if (m->tma()) return EE_OK;
+    const int64_t ld = (m->cols + 7) / 8 * 8;
+    uint16_t* p = (uint16_t*)c.mem.take((size_t)m->rows * ld * 2);
+    if (m->rows * (ld / 8) > (int64_t)0x7fffffff * 256) return fail(EE_EINVAL, "operand too large");
+    if (!c.dry) {
+        k_pack<<<n_blocks(m->rows * (ld / 8), 256), 256, 0, c.s>>>(m->p, m->ld, m->rows, m->cols, p, ld);
+        const int rc = cuda_status(cudaGetLastError());
+        if (rc != EE_OK) return rc;
+    }
+    m->p = p;
+    m->ld = ld;
+    return EE_OK;
+}
+
+bool make_map(CUtensorMap* map, const Mat& m, int type, int box_rows) {
+    auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(tensor_map_encoder());
+    if (!encode) return false;
+    const cuuint64_t dim[2] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows};
+    const cuuint64_t stride[1] = {(cuuint64_t)m.ld * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return encode(map, type == EE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                  const_cast<uint16_t*>(m.p), dim, stride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Tile width and k splits: the pair with the least estimated time.  A stage
+// costs its MMAs (2 BN cycles) or, for narrow tiles, about 260 cycles of copy;
+// a wave of items fills and drains the ring once (1500 cycles); splits write
+// and read their partial sums (about 2400 bytes a cycle over the whole GPU) and
+// take another launch (4000 cycles).
+struct Tiling {
+    int bn, S;
+};
+Tiling tiling(int64_t M, int64_t N, int nk, int n_sm) {
+    Tiling best{64, 1};
+    double best_t = 1e30;
+    for (int bn = 64; bn <= 256; bn *= 2)
+        for (int S = 1; S <= 32 && S <= (nk + 1) / 2; ++S) {
+            const int64_t items = (M + kTM - 1) / kTM * ((N + bn - 1) / bn) * S;
+            const double waves = (double)((items + n_sm - 1) / n_sm);
+            double t = waves * ((nk + S - 1) / S * std::max(2.0 * bn, 260.0) + 600) + 1500;
+            if (S > 1) t += 4000 + 8.0 * (double)S * M * N / 2400;
+            if (t < best_t) best_t = t, best = {bn, S};
+        }
+    return best;
+}
+
+template <int BN, bool A_MN, bool B_MN>
+int launch_gemm(const Ctx& c, const Mat& A, const Mat& B, const GemmArgs& g) {
+    CUtensorMap ma, mb;
+    if (!make_map(&ma, A, c.type, A_MN ? kTK : kTM) || !make_map(&mb, B, c.type, B_MN ? kTK : BN))
+        return fail(EE_ECUDA, "cuTensorMapEncodeTiled failed");
+    auto* k = k_gemm<BN, A_MN, B_MN>;
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GShape<BN>::smem);
+    if (e != cudaSuccess) return cuda_status(e);
+    const int64_t items = (int64_t)g.mt * g.nt * g.S;
+    k<<<(unsigned)std::min<int64_t>(items, c.n_sm), kGemmThreads, GShape<BN>::smem, c.s>>>(ma, mb, g);
+    return cuda_status(cudaGetLastError());
+}
+
+// D = A B^T.  A_MN / B_MN: the operand is stored with k as its rows.
+template <bool A_MN, bool B_MN>
+int gemm(Ctx& c, Mat A, Mat B, const Epilogue& e) {
+    int rc = aligned(c, &A);
+    if (rc == EE_OK) rc = aligned(c, &B);
+    if (rc != EE_OK) return rc;
+    GemmArgs g{};
+    const int64_t M = A_MN ? A.cols : A.rows, N = B_MN ? B.cols : B.rows, K = A_MN ? A.rows : A.cols;
+    if (M > 0x7fffff00 || N > 0x7fffff00) return fail(EE_EINVAL, "too many rows");
+    g.M = (int)M;
+    g.N = (int)N;
+    g.nk = (int)((K + kTK - 1) / kTK);
+    g.bf16 = c.type == EE_BF16;
+    const Tiling t = tiling(M, N, g.nk, c.n_sm);
+    g.mt = (int)((M + kTM - 1) / kTM);
+    g.nt = (int)((N + t.bn - 1) / t.bn);
+    g.S = t.S;
+    if ((int64_t)g.mt * g.nt * g.S > 0x7fffffff) return fail(EE_EINVAL, "too many rows");
+    g.ldp = (N + 7) / 8 * 8;
+    if (t.S > 1) g.part = (float*)c.mem.take(4 * (size_t)t.S * M * g.ldp);
+    g.e = e;
+    if (c.dry) return EE_OK;
+    rc = t.bn == 256 ? launch_gemm<256, A_MN, B_MN>(c, A, B, g)
+         : t.bn == 128 ? launch_gemm<128, A_MN, B_MN>(c, A, B, g)
+                       : launch_gemm<64, A_MN, B_MN>(c, A, B, g);
+    if (rc != EE_OK || t.S == 1) return rc;
+    k_join<<<n_blocks(M * (g.ldp / 8), 256), 256, 0, c.s>>>(g);
+    return cuda_status(cudaGetLastError());
+}
+
+template <int R, bool VEC>
+int launch_few(const ee_linear_args& a, const Ctx& c, const Epilogue& e) {
+    // outputs per warp: 4, or fewer when that would leave SMs without a CTA
+    const uint16_t *x = (const uint16_t*)a.x, *w = (const uint16_t*)a.w;
+    if (a.n_out >= 16 * 2 * c.n_sm && R <= 4)
+        k_linear_few<R, 4, VEC><<<n_blocks(a.n_out, 16), 128, 0, c.s>>>(x, a.ld_x, (int)a.rows, w, a.ld_w, a.n_in, a.n_out, e);
+    else if (a.n_out >= 8 * 2 * c.n_sm)
+        k_linear_few<R, 2, VEC><<<n_blocks(a.n_out, 8), 128, 0, c.s>>>(x, a.ld_x, (int)a.rows, w, a.ld_w, a.n_in, a.n_out, e);
+    else
+        k_linear_few<R, 1, VEC><<<n_blocks(a.n_out, 4), 128, 0, c.s>>>(x, a.ld_x, (int)a.rows, w, a.ld_w, a.n_in, a.n_out, e);
+    return cuda_status(cudaGetLastError());
+}
+
+int init(Ctx* c, void* scratch, bool dry, void* stream, int type) {
+    c->mem.base = dry ? nullptr : (char*)scratch;
+    c->dry = dry;
+    c->s = (cudaStream_t)stream;
+    c->type = type;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->n_sm, cudaDevAttrMultiProcessorCount, dev);
+    return cuda_status(e);
+}
+
+int check_mat(const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes) {
+    if (!p) return fail(EE_EINVAL, "NULL argument");
+    if (ld < cols && rows > 1) return fail(EE_EINVAL, "rows overlap: a row stride is below the width");
+    if ((uintptr_t)p % bytes) return fail(EE_EINVAL, "a tensor is not aligned to its type");
+    return EE_OK;
+}
+int check_shape(int type, int64_t rows, int n_in, int n_out, int act) {
+    if (type != EE_BF16 && type != EE_FP16) return fail(EE_EINVAL, "operands must be bf16 or fp16");
+    if (rows < 0 || rows > 0x7fffff00 || n_in < 1 || n_out < 1) return fail(EE_EINVAL, "bad shape");
+    if (act < EE_ACT_NONE || act > EE_ACT_GELU) return fail(EE_EINVAL, "unknown activation");
+    return EE_OK;
+}
+
+int check_forward(const ee_linear_args* a) {
+    if (!a) return fail(EE_EINVAL, "NULL argument");
+    int rc = check_shape(a->type, a->rows, a->n_in, a->n_out, a->activation);
+    if (rc != EE_OK) return rc;
+    if (a->out_type != a->type && a->out_type != EE_FP32) return fail(EE_EINVAL, "the result has the operands' type or fp32");
+    if (!a->rows) return EE_OK;
+    rc = check_mat(a->x, a->rows, a->n_in, a->ld_x, 2);
+    if (rc == EE_OK) rc = check_mat(a->w, a->n_out, a->n_in, a->ld_w, 2);
+    if (rc == EE_OK) rc = check_mat(a->out, a->rows, a->n_out, a->ld_out, bytes_of(a->out_type));
+    if (rc == EE_OK && a->residual) rc = check_mat(a->residual, a->rows, a->n_out, a->ld_residual, bytes_of(a->out_type));
+    if (rc == EE_OK && a->bias) rc = check_mat(a->bias, 1, a->n_out, a->n_out, 2);
+    if (rc == EE_OK && a->preact) rc = check_mat(a->preact, a->rows, a->n_out, a->n_out, 4);
+    return rc;
+}
+
+int forward(const ee_linear_args& a, Ctx& c) {
+    Epilogue e{};
+    e.bias = a.bias;
+    e.res = a.residual;
+    e.out = a.out;
+    e.preact = a.preact;
+    e.ld_res = a.ld_residual;
+    e.ld_out = a.ld_out;
+    e.ld_pre = a.n_out;
+    e.type = a.type;
+    e.out_type = a.out_type;
+    e.act = a.activation;
+    e.vec_bias = vec_ok(a.bias, 0, a.type);
+    e.vec_res = vec_ok(a.residual, a.ld_residual, a.out_type);
+    e.vec_out = vec_ok(a.out, a.ld_out, a.out_type);
+    e.vec_pre = vec_ok(a.preact, a.n_out, EE_FP32);
+    if (a.rows <= kFewRows) {
+        if (c.dry) return EE_OK;
+        const bool vec = vec_ok(a.x, a.ld_x, a.type) && vec_ok(a.w, a.ld_w, a.type);
+        if (a.rows == 1) return vec ? launch_few<1, true>(a, c, e) : launch_few<1, false>(a, c, e);
+        if (a.rows == 2) return vec ? launch_few<2, true>(a, c, e) : launch_few<2, false>(a, c, e);
+        if (a.rows <= 4) return vec ? launch_few<4, true>(a, c, e) : launch_few<4, false>(a, c, e);
+        return vec ? launch_few<8, true>(a, c, e) : launch_few<8, false>(a, c, e);
+    }
+    return gemm<false, false>(c, Mat{(const uint16_t*)a.x, a.rows, a.ld_x, a.n_in},
+                              Mat{(const uint16_t*)a.w, a.n_out, a.ld_w, a.n_in}, e);
+}
+
+int check_backward(const ee_linear_grad_args* a) {
+    if (!a) return fail(EE_EINVAL, "NULL argument");
+    int rc = check_shape(a->type, a->rows, a->n_in, a->n_out, a->activation);
+    if (rc != EE_OK) return rc;
+    if (!a->dx && !a->dw && !a->dbias) return fail(EE_EINVAL, "no gradient is asked for");
+    if (a->dw && a->dw_type != a->type && a->dw_type != EE_FP32)
+        return fail(EE_EINVAL, "the weight's gradient has the operands' type or fp32");
+    if (a->dw && (rc = check_mat(a->dw, a->n_out, a->n_in, a->n_in, bytes_of(a->dw_type))) != EE_OK) return rc;
+    if (a->dbias && (rc = check_mat(a->dbias, 1, a->n_out, a->n_out, 4)) != EE_OK) return rc;
+    if (!a->rows) return EE_OK;
+    rc = check_mat(a->dy, a->rows, a->n_out, a->ld_dy, 2);
+    if (rc == EE_OK && a->dx) rc = check_mat(a->dx, a->rows, a->n_in, a->ld_dx, 2);
+    if (rc == EE_OK && a->dx) rc = check_mat(a->w, a->n_out, a->n_in, a->ld_w, 2);
+    if (rc == EE_OK && a->dw) rc = check_mat(a->x, a->rows, a->n_in, a->ld_x, 2);
+    if (rc == EE_OK && a->activation != EE_ACT_NONE) rc = check_mat(a->preact, a->rows, a->n_out, a->n_out, 4);
+    return rc;
+}
+
+Epilogue plain_out(void* out, int64_t ld, int type, int out_type) {
+    Epilogue e{};
+    e.out = out;
+    e.ld_out = ld;
+    e.type = type;
+    e.out_type = out_type;
+    e.vec_out = vec_ok(out, ld, out_type);
+    return e;
+}
+
+int backward(const ee_linear_grad_args& a, Ctx& c) {
+    int rc = EE_OK;
+    Mat du{(const uint16_t*)a.dy, a.rows, a.ld_dy, a.n_out};
+    const bool act = a.activation != EE_ACT_NONE, products = a.dx || a.dw;
+    if (act || a.dbias) {
+        uint16_t* p = nullptr;
+        const int64_t ld = (a.n_out + 7) / 8 * 8;
+        if (act && products) p = (uint16_t*)c.mem.take((size_t)a.rows * ld * 2);
+        const int cols = n_blocks(a.n_out, 256);
+        const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 31) / 32, 4 * c.n_sm / cols));
+        float* part = a.dbias ? (float*)c.mem.take(4 * (size_t)blocks * a.n_out) : nullptr;
+        if (!c.dry) {
+            k_du<<<dim3(cols, blocks), 256, 0, c.s>>>(du.p, a.ld_dy, a.preact, a.n_out, a.rows, a.n_out, a.type,
+                                                      a.activation, vec_ok(a.dy, a.ld_dy, a.type),
+                                                      vec_ok(a.preact, a.n_out, EE_FP32), p, ld, part);
+            if (part) k_sum_blocks<<<n_blocks(a.n_out, 256), 256, 0, c.s>>>(part, blocks, a.n_out, a.dbias);
+            if ((rc = cuda_status(cudaGetLastError())) != EE_OK) return rc;
+        }
+        if (act && products) {
+            du.p = p;
+            du.ld = ld;
+        }
+    }
+    if (products && (rc = aligned(c, &du)) != EE_OK) return rc;
+    if (a.dx)
+        rc = gemm<false, true>(c, du, Mat{(const uint16_t*)a.w, a.n_out, a.ld_w, a.n_in},
+                               plain_out(a.dx, a.ld_dx, a.type, a.type));
+    if (rc == EE_OK && a.dw)
+        rc = gemm<true, true>(c, du, Mat{(const uint16_t*)a.x, a.rows, a.ld_x, a.n_in},
+                              plain_out(a.dw, a.n_in, a.type, a.dw_type));
+    return rc;
+}
+
+}  // namespace
+}  // namespace ee
+
+using namespace ee;
+
+extern "C" {
+
+int ee_linear_scratch_bytes(const ee_linear_args* args, size_t* bytes) {
+    int rc = check_forward(args);
+    if (rc != EE_OK) return rc;
+    if (!bytes) return fail(EE_EINVAL, "NULL argument");
+    Ctx c{};
+    if ((rc = init(&c, nullptr, true, nullptr, args->type)) != EE_OK) return rc;
+    if (args->rows && (rc = forward(*args, c)) != EE_OK) return rc;
+    *bytes = c.mem.at;
+    return EE_OK;
+}
+
+int ee_linear(const ee_linear_args* args, void* scratch, size_t scratch_bytes, void* stream) {
+    size_t need = 0;
+    int rc = ee_linear_scratch_bytes(args, &need);
+    if (rc != EE_OK || !args->rows) return rc;
+    if (need > scratch_bytes || (need && !scratch)) return fail(EE_ENOMEM, "scratch too small");
+    if ((uintptr_t)scratch % 256) return fail(EE_EINVAL, "scratch must be 256-byte aligned");
+    Ctx c{};
+    if ((rc = init(&c, scratch, false, stream, args->type)) != EE_OK) return rc;
+    return forward(*args, c);
+}
+
+int ee_linear_backward_scratch_bytes(const ee_linear_grad_args* args, size_t* bytes) {
+    int rc = check_backward(args);
+    if (rc != EE_OK) return rc;
+    if (!bytes) return fail(EE_EINVAL, "NULL argument");
+    Ctx c{};
+    if ((rc = init(&c, nullptr, true, nullptr, args->type)) != EE_OK) return rc;
+    if (args->rows && (rc = backward(*args, c)) != EE_OK) return rc;
+    *bytes = c.mem.at;
+    return EE_OK;
+}
+
+int ee_linear_backward(const ee_linear_grad_args* args, void* scratch, size_t scratch_bytes, void* stream) {
+    size_t need = 0;
+    int rc = ee_linear_backward_scratch_bytes(args, &need);
+    if (rc != EE_OK) return rc;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (!args->rows) {  // sums over no rows
+        cudaError_t e = cudaSuccess;
+        if (args->dw) e = cudaMemsetAsync(args->dw, 0, (size_t)args->n_out * args->n_in * bytes_of(args->dw_type), s);
+        if (e == cudaSuccess && args->dbias) e = cudaMemsetAsync(args->dbias, 0, 4 * (size_t)args->n_out, s);
+        return cuda_status(e);
+    }
+    if (need > scratch_bytes || (need && !scratch)) return fail(EE_ENOMEM, "scratch too small");
+    if ((uintptr_t)scratch % 256) return fail(EE_EINVAL, "scratch must be 256-byte aligned");
+    Ctx c{};
+    if ((rc = init(&c, scratch, false, stream, args->type)) != EE_OK) return rc;
+    return backward(*args, c);
+}
+
+}  // extern "C"

@@ -386,6 +386,8 @@ bool small_batch(int M) { return x3_rows(M) <= USmall::rows; }
 
 }  // namespace
 
+void* tensor_map_encoder() { return encode_fn() ? reinterpret_cast<void*>(g_encode) : nullptr; }
+
 bool configure_umma() {
     int dev = 0, major = 0;
     cudaGetDevice(&dev);

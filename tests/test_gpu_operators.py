@@ -1,0 +1,588 @@
+"""The operators that train and score a readout against their definitions in 64
+bits (needs a GB300): odd sizes, strides, alignments, masks and special values,
+gradients against the formulas and against differences."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+import paper_2609_14144_gb300 as ee  # noqa: E402
+
+BF16, FP16, FP32 = torch.bfloat16, torch.float16, torch.float32
+NAN, INF = float("nan"), float("inf")
+# half an ulp, relative, and the smallest step of the subnormals
+UNIT = {BF16: 2.0 ** -8, FP16: 2.0 ** -11, FP32: 2.0 ** -24}
+TINY = {BF16: 2.0 ** -133, FP16: 2.0 ** -24, FP32: 2.0 ** -149}
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def normal(g, rows, cols, dtype, std=1.0, pad=0, shift=0):
+    """rows x cols, its rows `pad` further apart than long, starting `shift` elements
+    after an aligned address; what lies around it is NaN."""
+    buf = torch.full((rows * (cols + pad) + shift + 8,), NAN, dtype=dtype, device="cuda")
+    t = buf[shift:shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    t.copy_(torch.randn((rows, cols), generator=g, device="cuda") * std)
+    return t
+
+
+def within(got, ref, bound, what=""):
+    """|got - ref| <= bound elementwise, NaN where and only where ref has one, and
+    equal infinities."""
+    got, ref = got.double(), ref.double()
+    bad = torch.isnan(got) != torch.isnan(ref)
+    assert not bad.any(), f"{what}: NaN differ at {bad.nonzero()[:4].tolist()}"
+    special = torch.isnan(ref) | torch.isinf(ref)
+    same = torch.where(torch.isinf(ref), got == ref, True)
+    assert same.all(), f"{what}: infinities differ"
+    err = torch.where(special, 0.0, (got - ref).abs())
+    over = err - torch.where(special, 0.0, torch.as_tensor(bound, dtype=torch.float64, device=ref.device).expand_as(ref))
+    assert (over <= 0).all(), f"{what}: error {err.flatten()[over.argmax()].item():.3e}, {over.max().item():.3e} over"
+
+
+def rounded(ref, dtype):
+    return ref.abs() * UNIT[dtype] + TINY[dtype]
+
+
+# ---------------------------------------------------------------- affine maps
+def act64(u, act):
+    return {None: lambda: u, "relu": lambda: u.clamp(min=0), "silu": lambda: u * torch.sigmoid(u),
+            "gelu": lambda: 0.5 * u * (1 + torch.erf(u / math.sqrt(2)))}[act]()
+
+
+def slope64(u, act):
+    s = torch.sigmoid(u)
+    return {None: lambda: torch.ones_like(u), "relu": lambda: (u > 0).double(), "silu": lambda: s * (1 + u * (1 - s)),
+            "gelu": lambda: 0.5 * (1 + torch.erf(u / math.sqrt(2))) + u * torch.exp(-u * u / 2) / math.sqrt(2 * math.pi)}[act]()
+
+
+def sum_bound(a, b, k):
+    """Products of 16-bit values are exact in 32 bits; a sum of k of them passes at
+    most 32 truncating steps of 16 in a chain (k / 512 chains) or k / 32 + 8 rounding
+    ones, each worth 2^-23 of the sum of magnitudes."""
+    return (64 + k / 32) * 2.0 ** -23 * (a.abs() @ b.abs())
+
+
+FORWARD = [(1, 1, 1), (1, 64, 64), (1, 1001, 2051), (2, 896, 688), (3, 7, 5), (5, 300, 4864), (8, 8960, 1536), (9, 64, 64),
+           (9, 1, 1), (37, 1001, 2051), (64, 896, 65), (128, 256, 256), (129, 72, 257), (300, 1536, 96), (515, 130, 1111),
+           (700, 520, 2000), (40, 12000, 33)]
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", FORWARD)
+@pytest.mark.parametrize("dtype,act,bias,res,out_dtype,pad,shift", [
+    (BF16, None, False, False, BF16, 0, 0), (FP16, "gelu", True, True, FP16, 3, 1), (BF16, "silu", True, False, FP32, 8, 0),
+    (FP16, "relu", False, True, FP32, 0, 3), (BF16, None, True, True, BF16, 1, 8)])
+def test_linear(rows, n_in, n_out, dtype, act, bias, res, out_dtype, pad, shift):
+    g = gen(rows * 7 + n_in)
+    x = normal(g, rows, n_in, dtype, 1.0, pad, shift)
+    w = normal(g, n_out, n_in, dtype, n_in ** -0.5, pad, shift)
+    b = normal(g, 1, n_out, dtype, 1.0, 0, shift)[0] if bias else None
+    r = normal(g, rows, n_out, out_dtype, 1.0, pad, shift) if res else None
+    out = normal(g, rows, n_out, out_dtype, 1.0, pad, shift)
+    y, pre = ee.linear(x, w, b, r, activation=act, out_dtype=out_dtype, keep_preact=True, out=out)
+    assert y is out
+    X, W = x.double(), w.double()
+    u = X @ W.t() + (b.double() if bias else 0)
+    tol = sum_bound(X, W.t(), n_in) + u.abs() * 2.0 ** -23
+    within(pre, u, tol, "preact")
+    ref = act64(u, act) + (r.double() if res else 0)
+    # slopes are below 1.13; exp, erf and the quotient a few units each
+    tol = 1.13 * tol + 16 * 2.0 ** -24 * (u.abs() + ref.abs())
+    within(y, ref, tol + rounded(ref.abs() + tol, out_dtype), "y")
+    # what lies between the rows of the result is not written
+    if pad and rows > 1:
+        assert torch.isnan(out.as_strided((rows - 1, pad), (n_out + pad, 1), out.storage_offset() + n_out)).all()
+    plain = ee.linear(x, w, b, r, activation=act, out_dtype=out_dtype)
+    assert torch.equal(plain, y)
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(1, 1, 1), (2, 896, 300), (9, 65, 33), (130, 257, 70), (513, 200, 1000), (1000, 64, 64),
+                                             (260, 5000, 129), (37, 130, 9000)])
+@pytest.mark.parametrize("dtype,act,dw_dtype,pad,shift", [(BF16, None, FP32, 0, 0), (FP16, None, FP16, 3, 1), (BF16, "silu", BF16, 8, 0),
+                                                          (FP16, "gelu", FP32, 0, 5), (BF16, "relu", BF16, 1, 0)])
+def test_linear_backward(rows, n_in, n_out, dtype, act, dw_dtype, pad, shift):
+    g = gen(rows * 11 + n_in)
+    x = normal(g, rows, n_in, dtype, 1.0, pad, shift)
+    w = normal(g, n_out, n_in, dtype, n_in ** -0.5, pad, shift)
+    dy = normal(g, rows, n_out, dtype, 1.0, pad, shift)
+    pre = torch.randn((rows, n_out), generator=g, device="cuda") if act else None
+    dx, dw, db = ee.linear_backward(dy, x, w, activation=act, preact=pre, dw_dtype=dw_dtype)
+    X, W, du = x.double(), w.double(), dy.double()
+    if act:
+        du = du * slope64(pre.double(), act)
+    # behind an activation du enters the products rounded to the operands' type
+    slack = du.abs() * (UNIT[dtype] + 32 * 2.0 ** -24) + TINY[dtype] if act else torch.zeros_like(du)
+    ref = du @ W
+    tol = slack @ W.abs() + sum_bound(du.abs() + slack, W, n_out)
+    within(dx, ref, tol + rounded(ref.abs() + tol, dtype), "dx")
+    ref = du.t() @ X
+    tol = slack.t() @ X.abs() + sum_bound(du.t().abs() + slack.t(), X, rows)
+    within(dw, ref, tol + rounded(ref.abs() + tol, dw_dtype), "dw")
+    within(db, du.sum(0), (rows + 40) * 2.0 ** -24 * du.abs().sum(0), "dbias")
+    # each alone gives the same
+    for i, name in enumerate(("dx", "dw", "dbias")):
+        kw = {n: n == name for n in ("dx", "dw", "dbias")}
+        only = ee.linear_backward(dy, x if name == "dw" else None, w if name != "dw" else None, activation=act, preact=pre,
+                                  dw_dtype=dw_dtype, **kw)
+        assert [t is None for t in only] == [j != i for j in range(3)]
+        assert torch.equal(only[i], (dx, dw, db)[i]), name
+
+
+@pytest.mark.parametrize("act", [None, "silu", "gelu"])
+def test_linear_gradients_against_differences(act):
+    """Directional derivative of sum(c * y) by central differences in 64 bits."""
+    g = gen(5)
+    rows, n_in, n_out, h = 40, 72, 56, 1e-5
+    x, w = normal(g, rows, n_in, BF16), normal(g, n_out, n_in, BF16, n_in ** -0.5)
+    b, c = normal(g, 1, n_out, BF16)[0], normal(g, rows, n_out, BF16)
+    _, pre = ee.linear(x, w, b, activation=act, keep_preact=True)
+    dx, dw, db = ee.linear_backward(c, x, w, activation=act, preact=pre, dw_dtype=FP32)
+    for got, at in ((dx, 0), (dw, 1), (db, 2)):
+        args = [x.double(), w.double(), b.double()]
+        d = torch.randn(args[at].shape, generator=g, device="cuda", dtype=torch.float64)
+
+        def f(sign):
+            a = list(args)
+            a[at] = a[at] + sign * h * d
+            return (c.double() * act64(a[0] @ a[1].t() + a[2], act)).sum()
+
+        want = ((f(1) - f(-1)) / (2 * h)).item()
+        have = (got.double() * d).sum().item()
+        # each element of the gradient is off by rounding (and du's); h^2 and 1e-16 / h are far below
+        scale = (got.double().abs() * d.abs()).sum().item()
+        assert abs(want - have) <= 3 * UNIT[BF16] * scale + 1e-5, (at, want, have)
+
+
+def test_linear_no_rows_and_reused_scratch():
+    w = torch.randn(64, 72, device="cuda").to(BF16)
+    x = torch.empty((0, 72), dtype=BF16, device="cuda")
+    assert ee.linear(x, w).shape == (0, 64)
+    dw = torch.full((64, 72), NAN, device="cuda", dtype=FP32)
+    dx, dw, db = ee.linear_backward(torch.empty((0, 64), dtype=BF16, device="cuda"), x, w, dw=dw, dw_dtype=FP32)
+    assert dx.shape == (0, 72) and not dw.any() and not db.any()
+    g = gen(3)  # scratch full of NaN, used by two calls in turn
+    mem = torch.full((1 << 22,), NAN, device="cuda")
+    x = normal(g, 100, 4001, BF16)
+    w = normal(g, 50, 4001, BF16, 0.02)
+    a, b = ee.linear(x, w, scratch=mem), ee.linear(x, w, scratch=mem)
+    assert torch.equal(a, b) and torch.equal(a, ee.linear(x, w)) and not torch.isnan(a).any()
+
+
+def test_linear_residual_in_place_and_other_stream():
+    g = gen(9)
+    x, w = normal(g, 200, 128, BF16), normal(g, 96, 128, BF16, 0.1)
+    r = normal(g, 200, 96, BF16)
+    want = ee.linear(x, w, residual=r)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    buf = r.clone()
+    s.wait_stream(torch.cuda.current_stream())
+    got = ee.linear(x, w, residual=buf, out=buf, stream=s)
+    s.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_linear_long_rows_do_not_drift():
+    """Sums of one sign: a truncating chain over the whole range would lose
+    k / 16 * 2^-24 of them."""
+    k = 65536
+    x = torch.rand((130, k), device="cuda").to(BF16)
+    w = torch.rand((70, k), device="cuda").to(BF16)
+    y = ee.linear(x, w, out_dtype=FP32)
+    ref = x.double() @ w.double().t()
+    assert ((y.double() - ref).abs() / ref).max().item() <= 2e-6
+
+
+def test_linear_nan_and_inf_stay_in_their_rows():
+    g = gen(4)
+    x, w = normal(g, 140, 80, BF16), normal(g, 70, 80, BF16)
+    x[3, 5], x[131, 79] = NAN, INF
+    y = ee.linear(x, w)
+    clean = [i for i in range(140) if i not in (3, 131)]
+    assert torch.isnan(y[3]).all() and not torch.isfinite(y[131]).any() and torch.isfinite(y[clean]).all()
+
+
+# ---------------------------------------------------------------- RMSNorm
+@pytest.mark.parametrize("rows,d", [(1, 1), (3, 7), (5, 896), (2, 2048), (700, 33), (4, 2049), (9, 4100), (3, 8192), (2, 8200), (2, 16384),
+                                    (1300, 256), (2500, 1536)])
+@pytest.mark.parametrize("tx,ty,tg,pad,shift", [(FP32, BF16, BF16, 0, 0), (BF16, BF16, BF16, 3, 1), (FP16, FP16, FP32, 8, 0),
+                                                (FP32, FP32, FP16, 1, 2)])
+def test_rms_norm(rows, d, tx, ty, tg, pad, shift):
+    g, eps = gen(rows + d), 1e-6
+    x = normal(g, rows, d, tx, 2.0, pad, shift)
+    gain = normal(g, 1, d, tg, 0.5, 0, shift)[0]
+    dy = normal(g, rows, d, ty, 1.0, pad, shift)
+    y, rstd = ee.rms_norm(x, gain, eps, out_dtype=ty)
+    dx, dg = ee.rms_norm_backward(dy, x, gain, rstd)
+    X, G, DY = x.double(), gain.double(), dy.double()
+    r = 1 / torch.sqrt(X.square().mean(-1, keepdim=True) + eps)
+    # a mean of squares passes d / 64 + 20 rounding steps of positive terms; r halves its relative error
+    rel = (d / 64 + 24) * 2.0 ** -24
+    within(rstd, r[:, 0], r[:, 0] * rel, "rstd")
+    ref = X * r * G
+    within(y, ref, ref.abs() * (rel + 4 * 2.0 ** -24) + rounded(ref, ty), "y")
+    gy, xh = DY * G, X * r
+    dot = (gy * xh).mean(-1, keepdim=True)
+    ref = r * (gy - xh * dot)
+    tol = r * (gy.abs() + xh.abs() * (dot.abs() + 2 * (gy * xh).abs().mean(-1, keepdim=True))) * 4 * rel
+    within(dx, ref, tol + rounded(ref.abs() + tol, tx), "dx")
+    within(dg, (DY * xh).sum(0), (DY * xh).abs().sum(0) * (rel + (rows + 8) * 2.0 ** -24), "dgain")
+    only_dx, none = ee.rms_norm_backward(dy, x, gain, rstd, dgain=False)
+    none2, only_dg = ee.rms_norm_backward(dy, x, gain, rstd, dx=False)
+    assert none is None and none2 is None and torch.equal(only_dx, dx) and torch.equal(only_dg, dg)
+    if tx == ty:  # in place
+        z = dy.clone()
+        ee.rms_norm_backward(z, x, gain, rstd, dx=z)
+        assert torch.equal(z, dx)
+        z = x.clone()
+        ee.rms_norm(z, gain, eps, out=z)
+        assert torch.equal(z, y)
+
+
+def test_rms_norm_against_differences_and_special_rows():
+    g, h, eps = gen(8), 1e-5, 1e-5
+    x, gain, c = normal(g, 30, 100, FP32), normal(g, 1, 100, FP32)[0], normal(g, 30, 100, FP32)
+    _, rstd = ee.rms_norm(x, gain, eps)
+    dx, dg = ee.rms_norm_backward(c, x, gain, rstd)
+    f = lambda X, G: (c.double() * X * torch.rsqrt(X.square().mean(-1, keepdim=True) + eps) * G).sum()  # noqa: E731
+    d = torch.randn(x.shape, generator=g, device="cuda", dtype=torch.float64)
+    X, G = x.double(), gain.double()
+    want = ((f(X + h * d, G) - f(X - h * d, G)) / (2 * h)).item()
+    assert abs(want - (dx.double() * d).sum().item()) <= 1e-4 * (dx.double() * d).abs().sum().item() / 30 + 1e-5
+    want = ((f(X, G + h * d[0]) - f(X, G - h * d[0])) / (2 * h)).item()
+    assert abs(want - (dg.double() * d[0]).sum().item()) <= 1e-4 * (dg.double() * d[0]).abs().sum().item()
+    x[0] = 0.0
+    x[1, 7] = NAN
+    y, rstd = ee.rms_norm(x, gain, eps)
+    assert not y[0].any() and abs(rstd[0].item() * math.sqrt(eps) - 1) < 1e-6 and torch.isnan(y[1]).all()
+    assert torch.isfinite(y[2:]).all()
+    y, _ = ee.rms_norm(torch.empty((0, 100), device="cuda"), gain, eps)
+    assert y.shape == (0, 100)
+    none = torch.empty((0, 100), device="cuda")
+    _, dg = ee.rms_norm_backward(none, none, gain, torch.empty(0, device="cuda"))
+    assert not dg.any()
+
+
+# ---------------------------------------------------------------- log probabilities
+def check_logprobs(z, ids, k, temperature):
+    lp, ent, lse, top, top_ids = ee.token_logprobs(z, ids, k=k, temperature=temperature)
+    Z, T, V = z.double(), float(torch.tensor(temperature, dtype=FP32)), z.shape[1]
+    m = Z.amax(-1, keepdim=True)
+    ref_lse = torch.logsumexp(Z / T, -1)
+    # (Z - lse would lose the sum where Z is the lowest value of a type)
+    ref = (Z - m) / T - torch.log(torch.exp((Z - m) / T).sum(-1, keepdim=True))
+    # powers to 2^-21 each, V / 256 + 30 steps of positive terms, and 32-bit values of the result's size
+    s = (V / 256 + 60) * 2.0 ** -24 + 2.0 ** -21
+    size = torch.nan_to_num(m[:, 0].abs() / T, 0, 0, 0) + 25
+    within(lse, ref_lse, s + 4 * 2.0 ** -24 * size, "lse")
+    p = torch.exp(ref)
+    within(ent, -torch.where(p > 0, p * ref, p * 0).sum(-1), 40 * s + 8 * 2.0 ** -24 * size, "entropy")
+    spread = lambda v: s + 6 * 2.0 ** -24 * (torch.nan_to_num((v - m / T).abs(), 0, 0, 0) + 25)  # noqa: E731
+    if ids is not None:
+        i = ids.long()
+        given = ref.gather(1, i.clamp(0, V - 1)[:, None])
+        tol = spread(given + ref_lse[:, None])[:, 0]
+        given = torch.where(i < 0, 0.0, torch.where(i >= V, NAN, given[:, 0]))
+        within(lp, given, tol, "logprob")
+    else:
+        assert lp is None
+    assert top.shape == top_ids.shape == (z.shape[0], k)
+    if k:
+        order = torch.sort(torch.where(torch.isnan(Z), INF, Z) + torch.where(torch.isnan(Z), 1.0, 0.0), dim=-1, descending=True,
+                           stable=True).indices
+        # NaN above +inf
+        nan_first = torch.sort(torch.isnan(Z.gather(1, order)).int(), dim=-1, descending=True, stable=True).indices
+        order = order.gather(1, nan_first)[:, :k]
+        assert torch.equal(top_ids.long(), order), "best tokens"
+        val = ref.gather(1, order)
+        within(top, val, spread(val + ref_lse[:, None]), "top_logprob")
+
+
+@pytest.mark.parametrize("rows,V,k", [(1, 1, 1), (1, 1, 0), (2, 5, 5), (3, 300, 128), (1, 4096, 8), (5, 50257, 20), (1, 151936, 20), (330, 1003, 64),
+                                      (400, 8192, 1), (2, 151936, 128), (1, 400000, 100), (700, 129, 17)])
+@pytest.mark.parametrize("dtype,T,pad,shift", [(BF16, 1.0, 0, 0), (FP16, 0.7, 47, 1), (FP32, 1.5, 0, 3), (BF16, 1.0, 1, 5)])
+def test_token_logprobs(rows, V, k, dtype, T, pad, shift):
+    g = gen(rows + V)
+    z = normal(g, rows, V, dtype, 3.0, pad, shift)
+    ids = torch.randint(0, V, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    ids[::3] = -1
+    ids[1::5] = V
+    check_logprobs(z, ids, k, T)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 400])
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+def test_token_logprobs_orders_ties_and_masks(rows, dtype):
+    """Rows that defeat the running bound (ascending, constant, few values), rows
+    with most or all tokens masked by -inf or by the type's lowest value."""
+    V, k, g = 20011, 64, gen(rows)
+    low = torch.finfo(dtype).min
+    base = normal(g, rows, V, FP32, 2.0)
+    forms = {
+        "ascending": torch.arange(V, device="cuda").float().expand(rows, V) / V * 20 - 10,
+        "descending": torch.arange(V, device="cuda").float().expand(rows, V) / V * -20,
+        "constant": torch.full((rows, V), 1.25, device="cuda"),
+        "zeros of both signs": torch.where(base > 0, 0.0, -0.0),
+        "three values": (base.clamp(-1, 1) * 1.4).round(),
+        "few allowed": torch.where(torch.arange(V, device="cuda") % 997 == 5, base, -INF),
+        "few allowed, lowest": torch.where(torch.arange(V, device="cuda") % 997 == 5, base, low),
+        "all lowest": torch.full((rows, V), low, device="cuda"),
+        "one": torch.where(torch.arange(V, device="cuda") == V - 1, 0.5, -INF).expand(rows, V),
+        "lowest and large": torch.where(base > 0, 60000.0, low),
+    }
+    ids = torch.full((rows,), 5, dtype=torch.int32, device="cuda")
+    for name, z in forms.items():
+        try:
+            check_logprobs(z.to(dtype).contiguous(), ids, k, 1.0)
+        except AssertionError as e:
+            raise AssertionError(f"{name}: {e}") from None
+
+
+@pytest.mark.parametrize("rows,V", [(1, 7), (2, 30011), (350, 1000)])
+def test_token_logprobs_special_rows(rows, V):
+    z = torch.full((rows, V), -INF, device="cuda")
+    ids = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    lp, ent, lse, top, top_ids = ee.token_logprobs(z, ids, k=5)
+    assert (lp == -INF).all() and (lse == -INF).all() and not ent.any() and (top == -INF).all()
+    assert torch.equal(top_ids, torch.arange(5, device="cuda", dtype=torch.int32).expand(rows, 5))
+    for special in (NAN, INF):  # a row holding one is NaN, its neighbours are not
+        z = torch.randn((rows + 1, V), generator=gen(1), device="cuda")
+        z[0, V // 2] = special
+        lp, ent, lse, top, top_ids = ee.token_logprobs(z, torch.zeros(rows + 1, dtype=torch.int32, device="cuda"), k=3)
+        assert torch.isnan(torch.stack([lp[0], ent[0], lse[0]])).all() and top_ids[0, 0].item() == V // 2
+        assert torch.isfinite(torch.stack([lp[1:], ent[1:], lse[1:]])).all()
+    z[0, :V // 2] = NAN
+    z[0, V // 2 + 1] = NAN
+    top_ids = ee.token_logprobs(z, k=5)[4]
+    want = [i for i in list(range(V // 2)) + [V // 2 + 1, V // 2]][:5]
+    assert top_ids[0].tolist() == want
+    lp, ent, lse, top, top_ids = ee.token_logprobs(torch.empty((0, V), device="cuda"), k=2)
+    assert ent.shape == (0,) and top.shape == (0, 2)
+
+
+# ---------------------------------------------------------------- distillation
+def teacher_list(g, z, k, T, tail):
+    t = (z.float() * 0.7 + torch.randn(z.shape, generator=g, device="cuda")) / T
+    top, idx = t.topk(k, -1)
+    return idx.to(torch.int32), (top - torch.logsumexp(t, -1, keepdim=True)) if tail else top + 3.0
+
+
+def distill64(z, ids, t, T, tail, weight=None):
+    Z, V, t = z.double() / T, z.shape[1], t.double()
+    i = ids.long()
+    here = (i >= 0) & (i < V) & (t != -INF)
+    t = torch.where(here, t, -INF)
+    none = (~here).all(-1, keepdim=True)
+    lq = t if tail else torch.where(none, -INF, t - torch.logsumexp(t, -1, keepdim=True))
+    q = torch.exp(lq)
+    lse = torch.logsumexp(Z, -1, keepdim=True)
+    lp = (Z - lse)
+    spare = torch.where(here, i, V)
+    at = torch.where(here, i, 0)
+    loss = torch.where(q > 0, q * (lq - lp.gather(1, at)), 0.0).sum(-1)
+    listed = torch.zeros((Z.shape[0], V + 1), dtype=torch.bool, device=Z.device).scatter_(1, spare, True)[:, :V]
+    full = torch.zeros((Z.shape[0], V + 1), dtype=torch.float64, device=Z.device).scatter_add_(1, spare, q)[:, :V]
+    total = q.sum(-1, keepdim=True)
+    grad = lp.exp() * total - full
+    if tail:
+        q0 = (1 - total).clamp(min=0)
+        q0 = torch.where(listed.all(-1, keepdim=True), 0.0, q0)
+        rest = torch.where(listed, -INF, Z)
+        lse0 = torch.logsumexp(rest, -1, keepdim=True)
+        loss = loss + torch.where(q0 > 0, q0 * (torch.log(q0) - (lse0 - lse)), 0.0)[:, 0]
+        grad = grad + q0 * (lp.exp() - torch.where(listed, 0.0, torch.exp(rest - lse0)))
+    grad = grad * T * (1.0 if weight is None else weight.double()[:, None])
+    return loss * T * T, grad
+
+
+def check_distill(z, ids, t, T, tail, weight, in_place=False):
+    V, k = z.shape[1], ids.shape[1]
+    ref, ref_g = distill64(z, ids, t, T, tail, weight)
+    loss, stats = ee.distill_topk(z, ids, t, temperature=T, tail=tail)
+    # log p to s (as for the log probabilities), weights q to a few units of size 1 together
+    span = (z.float().amax(-1) - z.float().amin(-1)).double().clamp(max=1e4) / T + 30
+    s = (V / 256 + k + 60) * 2.0 ** -24 + 2.0 ** -21
+    within(loss, ref, T * T * (4 * s + 16 * 2.0 ** -24 * span), "loss")
+    grad = ee.distill_topk_backward(weight, z, ids, t, stats, temperature=T, tail=tail)
+    # p and q to 8 s relative to 1 in a listed element; an unlisted one is a difference of two
+    # shares of its power, p (1 - q0 / p0)
+    p = torch.softmax(z.double() / T, -1)
+    wt = T * weight.double()[:, None].abs()
+    share = p
+    if tail:
+        i = ids.long()
+        here = (i >= 0) & (i < V) & (t != -INF)
+        listed = torch.zeros((z.shape[0], V + 1), dtype=torch.bool, device=z.device).scatter_(1, torch.where(here, i, V), True)[:, :V]
+        rest = torch.where(listed, -INF, z.double() / T)
+        share = p + torch.where(listed, 0.0, torch.nan_to_num(torch.exp(rest - torch.logsumexp(rest, -1, keepdim=True))))
+    full = distill64(z, ids, t, T, False)[1] * 0 + share
+    hit = (ref_g.abs() / wt.clamp(min=1e-30)) + full
+    tol = wt * hit * (8 * s + 16 * 2.0 ** -24 * span[:, None]) * 2
+    if tail:  # the unlisted share takes q0's absolute error, a few units of 1
+        tol = tol + wt * share * 32 * 2.0 ** -24
+    within(grad, ref_g, tol + rounded(ref_g.abs() + tol, z.dtype), "grad")
+    loss2, grad2 = ee.distill_topk_step(z, ids, t, weight, temperature=T, tail=tail)
+    assert torch.equal(loss, loss2)
+    within(grad2, ref_g, tol + rounded(ref_g.abs() + tol, z.dtype), "step grad")
+    if in_place:
+        a, b = z.clone(), z.clone()
+        assert torch.equal(ee.distill_topk_step(a, ids, t, weight, temperature=T, tail=tail, grad=a)[1], grad2)
+        assert torch.equal(ee.distill_topk_backward(weight, b, ids, t, stats, temperature=T, tail=tail, grad=b), grad)
+
+
+@pytest.mark.parametrize("rows,V,k", [(1, 1, 1), (2, 5, 5), (3, 300, 128), (7, 4096, 8), (5, 50257, 17), (1, 151936, 64), (330, 1003, 64), (2, 400000, 3),
+                                      (700, 129, 17)])
+@pytest.mark.parametrize("dtype,T,pad,shift", [(BF16, 1.0, 0, 0), (FP16, 2.0, 47, 1), (FP32, 1.5, 0, 3), (BF16, 1.0, 1, 5)])
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill(rows, V, k, dtype, T, pad, shift, tail):
+    g = gen(rows + V)
+    z = normal(g, rows, V, dtype, 3.0, pad, shift)
+    ids, t = teacher_list(g, z, k, T, tail)
+    if k > 2:
+        ids[::2, k // 2] = -1
+        ids[1::4, 0] = V
+        t[::3, 1] = -INF
+    w = torch.rand(rows, generator=g, device="cuda") + 0.5
+    w[2::5] = 0.0
+    check_distill(z, ids, t, T, tail, w, in_place=pad == 0 and shift == 0)
+
+
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_gradient_against_differences(tail):
+    g, h = gen(2), 1e-5
+    z = normal(g, 6, 200, FP32, 2.0)
+    ids, t = teacher_list(g, z, 9, 1.0, tail)
+    w = torch.rand(6, generator=g, device="cuda") + 0.5
+    _, grad = ee.distill_topk_step(z, ids, t, w, tail=tail)
+    for _ in range(3):
+        d = torch.randn(z.shape, generator=g, device="cuda", dtype=torch.float64)
+        f = lambda s: (w.double() * distill64(z.double() + s * h * d, ids, t, 1.0, tail)[0]).sum()  # noqa: E731
+        want = ((f(1) - f(-1)) / (2 * h)).item()
+        assert abs(want - (grad.double() * d).sum().item()) <= 1e-5 * (grad.double() * d).abs().sum().item() + 1e-6
+
+
+def test_distill_listed_twice_and_list_strides():
+    g = gen(6)
+    z = normal(g, 20, 1000, FP32, 2.0)
+    wide_ids, wide_t = teacher_list(g, z, 12, 1.0, False)
+    ids, t = wide_ids[:, :7], wide_t[:, :7]  # rows of a wider list
+    ids[:, 3] = ids[:, 0]
+    ids[4:9, 5] = ids[4:9, 0]
+    w = torch.ones(20, device="cuda")
+    check_distill(z, ids, t, 1.0, False, w)
+    t = t - 6.0  # as log probabilities that leave something over
+    check_distill(z, ids, t, 1.0, True, w)
+
+
+@pytest.mark.parametrize("rows,V", [(2, 30011), (400, 1000)])
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_special_rows(rows, V, tail):
+    g = gen(V)
+    z = normal(g, rows, V, FP32, 2.0)
+    ids, t = teacher_list(g, z, 6, 1.0, tail)
+    w = torch.ones(rows, device="cuda")
+    # an empty list: nothing to learn
+    none = torch.full_like(ids, -1)
+    loss, grad = ee.distill_topk_step(z, none, t, w, tail=tail)
+    assert loss.abs().max().item() <= 1e-6 and grad.abs().max().item() <= 1e-6
+    # a row of weight 0 may hold anything
+    bad = z.clone()
+    bad[0] = NAN
+    zero = w.clone()
+    zero[0] = 0.0
+    loss, grad = ee.distill_topk_step(bad, ids, t, zero, tail=tail)
+    assert not grad[0].any() and torch.isfinite(grad[1:]).all() and torch.isfinite(loss[1:]).all()
+    loss, stats = ee.distill_topk(bad, ids, t, tail=tail)
+    assert torch.isnan(loss[0])
+    assert not ee.distill_topk_backward(zero, bad, ids, t, stats, tail=tail)[0].any()
+    # a row without a finite logit
+    bad[0] = -INF
+    loss, grad = ee.distill_topk_step(bad, ids, t, w, tail=tail)
+    assert loss[0].item() == INF and not grad[0].any() and torch.isfinite(grad).all() and torch.isfinite(loss[1:]).all()
+    # a confident student: the rest of the vocabulary is far below one ulp of its sum
+    sure = z.clone()
+    sure[:, 3] = 95.0
+    check_distill(sure, ids, t, 1.0, tail, w)
+    # the tokens outside the list masked out, with a teacher that leaves nothing over
+    masked = torch.full_like(z, -INF).scatter_(1, ids.long(), z.gather(1, ids.long()))
+    t1 = torch.log_softmax(t, -1)
+    loss, grad = ee.distill_topk_step(masked, ids, t1, w, tail=tail)
+    ref, ref_g = distill64(masked, ids, t1, 1.0, False, w)
+    within(loss, ref, 1e-5, "masked loss")
+    within(grad, ref_g, 1e-6, "masked grad")
+    # no rows
+    e = torch.empty((0, V), device="cuda")
+    loss, grad = ee.distill_topk_step(e, ids[:0], t[:0], w[:0], tail=tail)
+    assert loss.shape == (0,) and grad.shape == (0, V)
+
+
+def test_results_do_not_change_from_call_to_call():
+    g = gen(12)
+    z = normal(g, 40, 50257, BF16, 3.0)
+    ids, t = teacher_list(g, z, 30, 1.0, True)
+    x, w = normal(g, 300, 640, BF16), normal(g, 200, 640, BF16)
+    a = [*ee.token_logprobs(z, None, k=50)[1:], *ee.distill_topk_step(z, ids, t, tail=True), *ee.linear_backward(ee.linear(x, w), x, w),
+         *ee.rms_norm_backward(x, x, x[0], torch.ones(300, device="cuda"))]
+    for _ in range(3):
+        b = [*ee.token_logprobs(z, None, k=50)[1:], *ee.distill_topk_step(z, ids, t, tail=True), *ee.linear_backward(ee.linear(x, w), x, w),
+             *ee.rms_norm_backward(x, x, x[0], torch.ones(300, device="cuda"))]
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_operators_run_in_a_captured_graph():
+    g = gen(13)
+    x, w = normal(g, 64, 256, BF16), normal(g, 1000, 256, BF16, 0.1)
+    ids, t = torch.zeros((64, 2), dtype=torch.int32, device="cuda"), torch.zeros((64, 2), device="cuda")
+    ids[:, 1] = 7
+
+    def step():
+        y = ee.linear(x, w)
+        loss, grad = ee.distill_topk_step(y, ids, t)
+        return loss, ee.linear_backward(grad, x, w)[1], ee.token_logprobs(y, k=4)[4]
+
+    want = step()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+def test_refusals():
+    x, w = torch.zeros((4, 16), dtype=BF16, device="cuda"), torch.zeros((8, 16), dtype=BF16, device="cuda")
+    z = torch.zeros((4, 100), device="cuda")
+    ids, t = torch.zeros((4, 3), dtype=torch.int32, device="cuda"), torch.zeros((4, 3), device="cuda")
+    one = torch.ones(4, device="cuda")
+    for call in (lambda: ee.linear(x, w[:, :8]), lambda: ee.linear(x, w.half()), lambda: ee.linear(x, w, x[0, :7]),
+                 lambda: ee.linear(x, w, activation="tanh"), lambda: ee.linear(x.cpu(), w), lambda: ee.linear(x.t(), w),
+                 lambda: ee.linear(x, w, residual=torch.zeros((4, 7), dtype=BF16, device="cuda")),
+                 lambda: ee.linear(x, w, scratch=w, out=z), lambda: ee.linear_backward(x[:, :8], None, None),
+                 lambda: ee.linear_backward(x[:, :8], x, w, activation="silu"), lambda: ee.linear_backward(x[:, :8], None, w),
+                 lambda: ee.rms_norm(x, w[0, :9], 1e-6), lambda: ee.rms_norm(x.long(), w[0], 1e-6),
+                 lambda: ee.rms_norm_backward(x, x, w[0], one[:3]), lambda: ee.token_logprobs(z, ids[:, 0].long()),
+                 lambda: ee.token_logprobs(z[0]), lambda: ee.token_logprobs(z.double()), lambda: ee.distill_topk(z, ids.long(), t),
+                 lambda: ee.distill_topk(z, ids, t[:, :2]), lambda: ee.distill_topk_step(z, ids, t, one[:2]),
+                 lambda: ee.distill_topk_step(z, ids, t, grad=z.half()), lambda: ee.distill_topk_backward(one, z, ids, t, one)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: ee.linear(x.float(), w.float()), lambda: ee.linear(x[:1].expand(4, 16), w),
+                 lambda: ee.rms_norm(x, w[0], -1.0), lambda: ee.rms_norm(torch.zeros((1, 16385), device="cuda"), torch.zeros(16385, device="cuda"), 0.0),
+                 lambda: ee.rms_norm_backward(x, x, w[0], one, dx=False, dgain=False), lambda: ee.token_logprobs(z, k=101),
+                 lambda: ee.token_logprobs(z, k=-1), lambda: ee.token_logprobs(torch.zeros((1, 200), device="cuda"), k=129),
+                 lambda: ee.token_logprobs(z, temperature=0.0), lambda: ee.token_logprobs(z, temperature=NAN),
+                 lambda: ee.token_logprobs(z[:1].expand(4, 100)), lambda: ee.distill_topk(z, ids, t, temperature=-1.0),
+                 lambda: ee.distill_topk(z, ids[:, :0], t[:, :0])):
+        with pytest.raises(ee.EEError) as e:
+            call()
+        assert e.value.code == -1
+    torch.cuda.synchronize()

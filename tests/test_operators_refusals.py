@@ -1,0 +1,100 @@
+"""The C entries of the operators refuse bad arguments before they touch a device
+(no GPU)."""
+import ctypes
+
+import pytest
+
+from paper_2609_14144_gb300 import _lib
+
+P = 4096  # an aligned address that is never read: every call below is refused
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return _lib.load(allow_build=True)
+
+
+def refused(rc):
+    assert rc == _lib.EE_EINVAL, rc
+    assert _lib.load().ee_last_error()
+
+
+def linear_args(**kw):
+    a = dict(type=0, out_type=0, activation=0, n_in=16, n_out=8, rows=4, x=P, ld_x=16, w=P, ld_w=16, bias=None, residual=None,
+             ld_residual=8, out=P, ld_out=8, preact=None)
+    a.update(kw)
+    return _lib.LinearArgs(**a)
+
+
+@pytest.mark.parametrize("bad", [dict(type=2), dict(type=7), dict(out_type=1), dict(activation=4), dict(activation=-1), dict(n_in=0), dict(n_out=-3),
+                                 dict(rows=-1), dict(x=None), dict(w=None), dict(out=None), dict(ld_x=15), dict(ld_w=8), dict(ld_out=7),
+                                 dict(residual=P, ld_residual=3), dict(x=P + 1), dict(out_type=2, out=P + 2), dict(preact=P + 2)])
+def test_linear(lib, bad):
+    nb = ctypes.c_size_t(0)
+    a = linear_args(**bad)
+    refused(lib.ee_linear_scratch_bytes(ctypes.byref(a), ctypes.byref(nb)))
+    refused(lib.ee_linear(ctypes.byref(a), None, 0, None))
+
+
+def test_linear_null_structures(lib):
+    nb = ctypes.c_size_t(0)
+    refused(lib.ee_linear_scratch_bytes(None, ctypes.byref(nb)))
+    refused(lib.ee_linear(None, None, 0, None))
+    refused(lib.ee_linear_backward_scratch_bytes(None, ctypes.byref(nb)))
+    refused(lib.ee_linear_backward(None, None, 0, None))
+    a = linear_args()
+    refused(lib.ee_linear_scratch_bytes(ctypes.byref(a), None))
+
+
+@pytest.mark.parametrize("bad", [dict(type=2), dict(activation=9), dict(dx=None, dw=None, dbias=None), dict(dw_type=1), dict(rows=-2), dict(dy=None),
+                                 dict(x=None), dict(w=None), dict(activation=2), dict(ld_dy=3), dict(ld_dx=3), dict(dbias=P + 2), dict(n_in=0)])
+def test_linear_backward(lib, bad):
+    a = dict(type=0, activation=0, n_in=16, n_out=8, rows=4, dy=P, ld_dy=8, x=P, ld_x=16, w=P, ld_w=16, preact=None, dx=P, ld_dx=16,
+             dw=P, dw_type=2, reserved=0, dbias=P)
+    a.update(bad)
+    a = _lib.LinearGradArgs(**a)
+    nb = ctypes.c_size_t(0)
+    refused(lib.ee_linear_backward_scratch_bytes(ctypes.byref(a), ctypes.byref(nb)))
+    refused(lib.ee_linear_backward(ctypes.byref(a), None, 0, None))
+
+
+def test_rms_norm(lib):
+    def fwd(x=P, xt=0, rows=4, d=16, ld=16, gain=P, gt=0, eps=1e-6, y=P, yt=0, ldy=16):
+        return lib.ee_rms_norm(x, xt, rows, d, ld, gain, gt, eps, y, yt, ldy, None, None)
+
+    for bad in (dict(x=None), dict(xt=3), dict(rows=-1), dict(d=0), dict(d=16385, ld=16385, ldy=16385), dict(ld=15), dict(gain=None), dict(gt=-1),
+                dict(eps=-1.0), dict(eps=float("nan")), dict(y=None), dict(yt=5), dict(ldy=2), dict(x=P + 1), dict(yt=2, y=P + 2)):
+        refused(fwd(**bad))
+
+    def bwd(dy=P, x=P, rows=4, d=16, rstd=P, dx=P, dgain=P, ldx=16):
+        return lib.ee_rms_norm_backward(dy, 0, 16, x, 0, rows, d, ldx, P, 0, rstd, dx, 16, dgain, None, 0, None)
+
+    for bad in (dict(dy=None), dict(x=None), dict(rows=-1), dict(d=0), dict(rstd=None), dict(dx=None, dgain=None), dict(ldx=3)):
+        refused(bwd(**bad))
+    refused(lib.ee_rms_norm_scratch_bytes(4, 0, ctypes.byref(ctypes.c_size_t(0))))
+    refused(lib.ee_rms_norm_scratch_bytes(4, 16, None))
+
+
+def test_token_logprobs(lib):
+    def call(z=P, t=2, rows=4, vocab=100, ld=100, ids=P, k=3, temp=1.0, lp=P, tl=P, ti=P):
+        return lib.ee_token_logprobs(z, t, rows, vocab, ld, ids, k, temp, lp, P, P, tl, ti, None)
+
+    for bad in (dict(z=None), dict(t=3), dict(rows=-1), dict(vocab=0), dict(vocab=(1 << 23) + 1, ld=1 << 24), dict(ld=99), dict(ids=None), dict(k=-1),
+                dict(k=129, vocab=1000, ld=1000), dict(k=101), dict(temp=0.0), dict(temp=-1.0), dict(temp=float("nan")),
+                dict(temp=float("inf")), dict(tl=None), dict(ti=None), dict(z=P + 2)):
+        refused(call(**bad))
+
+
+def test_distill(lib):
+    def fwd(z=P, t=2, rows=4, vocab=100, ld=100, ids=P, ldi=3, tch=P, ldt=3, k=3, temp=1.0, loss=P, stats=P, grad=P, ldg=100):
+        return lib.ee_distill_topk(z, t, rows, vocab, ld, ids, ldi, tch, ldt, k, temp, 0, loss, stats, None, grad, ldg, None)
+
+    for bad in (dict(z=None), dict(t=-1), dict(rows=-1), dict(vocab=0), dict(ld=99), dict(ids=None), dict(ldi=2), dict(tch=None), dict(ldt=0), dict(k=0),
+                dict(k=129, ldi=200, ldt=200), dict(temp=0.0), dict(loss=None), dict(stats=P + 4), dict(ldg=99), dict(grad=P + 2)):
+        refused(fwd(**bad))
+
+    def bwd(dl=P, z=P, stats=P, grad=P, k=3, ldg=100):
+        return lib.ee_distill_topk_backward(dl, z, 2, 4, 100, 100, P, 3, P, 3, k, 1.0, 0, stats, grad, ldg, None)
+
+    for bad in (dict(dl=None), dict(z=None), dict(stats=None), dict(stats=P + 8), dict(grad=None), dict(k=0), dict(ldg=1)):
+        refused(bwd(**bad))
