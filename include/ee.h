@@ -451,6 +451,8 @@ int ee_select_tau(const float* conf, int conf_stride, const int32_t* member, int
 #define EE_MAX_TOP 128        /* entries of a list of best tokens */
 #define EE_MAX_VOCAB (1 << 23)
 #define EE_MAX_NORM 16384     /* width of ee_rms_norm */
+#define EE_MIN_TEMPERATURE 1e-4f
+#define EE_MAX_TEMPERATURE 100.0f
 
 /* y = act(x W^T + b) + r for x [rows, n_in], W [n_out, n_in], b [n_out], r and
  * y [rows, n_out].  x, W and b have type EE_BF16 or EE_FP16 (`type`); y and r

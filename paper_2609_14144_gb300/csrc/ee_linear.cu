@@ -20,6 +20,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "ee_internal.h"
 #include "ee_umma.cuh"
@@ -116,6 +117,9 @@ struct Epilogue {
     int64_t ld_res, ld_out, ld_pre;
     int type, out_type, act;
     bool vec_bias, vec_res, vec_out, vec_pre;  // 16-byte access at multiples of 8 columns
+    bool vec_all() const {
+        return vec_out && (!bias || vec_bias) && (!res || vec_res) && (!preact || vec_pre);
+    }
 };
 __device__ __forceinline__ void emit8(const Epilogue& e, int64_t row, int64_t col, int n, float (&v)[8]) {
     if (e.bias) {
@@ -136,6 +140,39 @@ __device__ __forceinline__ void emit8(const Epilogue& e, int64_t row, int64_t co
         for (int i = 0; i < 8; ++i) v[i] += r[i];
     }
     store8((char*)e.out + (row * e.ld_out + col) * bytes_of(e.out_type), e.out_type, n, e.vec_out, v);
+}
+
+// The same without an activation for four rows, row0 + 8 i, of a block whose
+// 16-byte accesses are all in range and aligned: each step is done for the four
+// together, so that their accesses are in flight at the same time.
+__device__ __forceinline__ void emit8x4(const Epilogue& e, int64_t row0, int64_t col, float (&v)[4][8]) {
+    float t[4][8];
+    if (e.res) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            load8((const char*)e.res + ((row0 + 8 * i) * e.ld_res + col) * bytes_of(e.out_type), e.out_type, 8, true, t[i]);
+    }
+    if (e.bias) {
+        float b[8];
+        load8((const char*)e.bias + col * 2, e.type, 8, true, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[i][k] += b[k];
+    }
+    if (e.preact) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store8(e.preact + (row0 + 8 * i) * e.ld_pre + col, EE_FP32, 8, true, v[i]);
+    }
+    if (e.res) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[i][k] += t[i][k];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        store8((char*)e.out + ((row0 + 8 * i) * e.ld_out + col) * bytes_of(e.out_type), e.out_type, 8, true, v[i]);
 }
 
 // ---------------------------------------------------------------- few rows
@@ -190,15 +227,18 @@ __global__ void __launch_bounds__(128) k_linear_few(const uint16_t* __restrict__
 
 // ---------------------------------------------------------------- tensor cores
 constexpr int kTM = 128, kTK = 64;        // tile rows; k per stage: 128 bytes
-constexpr int kChain = 8;                 // stages the tensor core adds up by itself
 constexpr int kEpiWarps = 8;
 constexpr int kGemmThreads = 32 * (4 + kEpiWarps);
 constexpr int kABytes = kTM * kTK * 2;
 
-template <int BN>
+// PAIR: two CTAs of a cluster share a tile of 256 rows (cta_group::2).  Each
+// stages its own 128 rows of A and half of B's, 32 KB a stage instead of 48 for
+// the same work per SM, and holds its rows' sums.
+template <int BN, bool PAIR>
 struct GShape {
-    static constexpr int b_bytes = BN * kTK * 2, stage = kABytes + b_bytes;
-    static constexpr int ST = 196608 / stage;  // 4, 6 or 8 stages in 192 KB
+    static constexpr int CG = PAIR ? 2 : 1;
+    static constexpr int b_rows = BN / CG, stage = kABytes + b_rows * kTK * 2;
+    static constexpr int ST = 196608 / stage;  // 4 to 8 stages in 192 KB
     static constexpr int tmem = 2 * BN;        // two accumulators
     static constexpr size_t smem = (size_t)ST * stage + kEpiWarps * 4096 + 1024 + 512;
 };
@@ -216,21 +256,72 @@ __device__ __forceinline__ uint64_t sw128_desc(uint32_t saddr, bool mn) {
     return d;
 }
 
-__device__ __forceinline__ void tma_2d(void* dst, const CUtensorMap* map, int c0, int c1, uint64_t* bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-            u_saddr(dst)),
-        "l"(map), "r"(c0), "r"(c1), "r"(u_saddr(bar))
-        : "memory");
+// bar: a shared::cluster address; in a pair it may be the other CTA's.
+template <bool PAIR>
+__device__ __forceinline__ void tma_2d(void* dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
+    if constexpr (PAIR)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], "
+            "[%4];" ::"r"(u_saddr(dst)),
+            "l"(map), "r"(c0), "r"(c1), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+                u_saddr(dst)),
+            "l"(map), "r"(c0), "r"(c1), "r"(bar)
+            : "memory");
 }
 __device__ __forceinline__ void expect_tx(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(u_saddr(bar)), "r"(bytes) : "memory");
+}
+// The address of the pair's first CTA's copy of p.
+__device__ __forceinline__ uint32_t leader_addr(const void* p) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(u_saddr(p)));
+    return r;
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void mma(uint32_t tmem_d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (PAIR)
+        asm volatile(
+            "{ .reg .pred p; setp.ne.u32 p, %4, 0; tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p; }" ::"r"(tmem_d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        u_mma(tmem_d, a, b, idesc, accumulate);
+}
+// One lane of the converged warp, always the same.
+__device__ __forceinline__ bool elect() {
+    uint32_t p;
+    asm volatile("{ .reg .pred p; elect.sync _|p, 0xffffffff; selp.u32 %0, 1, 0, p; }" : "=r"(p));
+    return p != 0;
+}
+// Arrives once the MMAs issued so far are complete: in a pair on both CTAs' copies.
+template <bool PAIR>
+__device__ __forceinline__ void commit(uint64_t* bar) {
+    if constexpr (PAIR)
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                u_saddr(bar)),
+            "h"((uint16_t)3)
+            : "memory");
+    else
+        u_commit(bar);
 }
 
 struct GemmArgs {
     int M, N, nk;        // nk: stages over the whole k range
     int mt, nt, S;       // tiles, k splits
-    int bf16;
+    int chain;           // stages the tensor core adds up by itself
+    bool bf16, vec;
     float* part;         // S > 1: partial sums [S][M][ldp]
     int64_t ldp;
     Epilogue e;
@@ -238,17 +329,22 @@ struct GemmArgs {
 
 // A persistent CTA per SM.  Warp 0 feeds the ring of stages by TMA, warp 1
 // issues the MMAs, warps 4 to 11 read the accumulators back.  A work item is
-// one tile over one k split; its stages are issued in chains of 8 into two
+// one tile over one k split; its stages are issued in chains into two
 // tensor-memory accumulators in turn, and each chain is added to the item's
 // sums in registers, rounding to nearest: the tensor core truncates as it adds,
 // so a long range in one chain would drift (the error grows with its steps).
 // The next chain, or the next item's first, runs while one is read back.
+// Reading a chain back slows the MMAs beside it by about 600 cycles (measured
+// with chains of 8 stages, 640 cycles each): results of 32 bits take chains of 8
+// (k = 512), results of 16 bits chains of 32, whose drift of at most 128 * 2^-23
+// is far below their rounding.
 // A wait that runs out (about 2 s) ends the CTA's loops; its remaining items
 // are written as NaN.
-template <int BN, bool A_MN, bool B_MN>
+template <int BN, bool PAIR, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_gemm(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, GemmArgs g) {
-    using G = GShape<BN>;
+    using G = GShape<BN, PAIR>;
+    constexpr int CG = G::CG;
     extern __shared__ __align__(1024) uint8_t g_smem_raw[];
     uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(g_smem_raw) + 1023) & ~(uintptr_t)1023);
     float* stage_out = reinterpret_cast<float*>(sm + G::ST * G::stage);
@@ -259,7 +355,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     uint64_t* done = acc_empty + 2;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
     volatile int* stall = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    const int w = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int w = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
         for (int i = 0; i < G::ST; ++i) {
             u_mb_init(&full[i], 1);
@@ -267,112 +363,137 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         }
         for (int i = 0; i < 2; ++i) {
             u_mb_init(&acc_full[i], 1);
-            u_mb_init(&acc_empty[i], kEpiWarps);
+            u_mb_init(&acc_empty[i], kEpiWarps * CG);
         }
         u_mb_init(done, 1);
         *stall = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (w == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(u_saddr(tmem_slot)),
-                     "r"(G::tmem)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(u_saddr(tmem_slot)),
+                         "r"(G::tmem)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(u_saddr(tmem_slot)),
+                         "r"(G::tmem)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     u_fence_before();
     __syncthreads();
+    if (PAIR) cluster_barrier();  // both CTAs' barriers are set up, both have their tensor memory
     u_fence_after();
     const uint32_t tmem = *tmem_slot;
+    const int rank = PAIR ? (int)(blockIdx.x & 1) : 0;
+    const int first = blockIdx.x / CG, stride = gridDim.x / CG;
     const int tiles = g.mt * g.nt, items = tiles * g.S;
 
     if (w < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
-        if (w == 0 && lane == 0) {  // producer
-            int64_t i = 0;
-            bool ok = true;
-            for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
-                const int tile = it % tiles, s = it / tiles, m0 = tile % g.mt * kTM, n0 = tile / g.mt * BN;
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        // Both issuing warps step through their stages as a whole and elect a lane
+        // for the copies and MMAs, so that addresses and descriptors stay in uniform
+        // registers: with one thread in the loop a stage took 600 cycles to issue.
+        if (w == 0) {  // producer
+            int st = 0, ph = 0;
+            bool ok = true, lap = false;
+            for (int it = first; it < items && ok; it += stride) {
+                const int tile = it % tiles, s = it / tiles;
+                const int m0 = (tile % g.mt * CG + rank) * kTM, n0 = tile / g.mt * BN + rank * G::b_rows;
                 const int k0 = (int)((int64_t)g.nk * s / g.S), k1 = (int)((int64_t)g.nk * (s + 1) / g.S);
-                for (int k = k0; k < k1; ++k, ++i) {
-                    const int st = (int)(i % G::ST);
-                    if (i >= G::ST && !u_mb_wait(&empty[st], (int)(i / G::ST - 1) & 1, stall)) {
+                for (int k = k0; k < k1; ++k) {
+                    if (lap && !__all_sync(kFull, u_mb_wait(&empty[st], ph ^ 1, stall))) {
                         *stall = kErrStall;
                         ok = false;
                         break;
                     }
                     uint8_t* a = sm + st * G::stage;
                     uint8_t* b = a + kABytes;
-                    expect_tx(&full[st], G::stage);
-                    if (A_MN) {
+                    if (elect()) {
+                        if (rank == 0) expect_tx(&full[st], G::stage * CG);
+                        const uint32_t bar = PAIR ? leader_addr(&full[st]) : u_saddr(&full[st]);
+                        if (A_MN) {
 #pragma unroll
-                        for (int j = 0; j < kTM / 64; ++j) tma_2d(a + j * kTK * 128, &ma, m0 + 64 * j, k * kTK, &full[st]);
-                    } else
-                        tma_2d(a, &ma, k * kTK, m0, &full[st]);
-                    if (B_MN) {
+                            for (int j = 0; j < kTM / 64; ++j) tma_2d<PAIR>(a + j * kTK * 128, &ma, m0 + 64 * j, k * kTK, bar);
+                        } else
+                            tma_2d<PAIR>(a, &ma, k * kTK, m0, bar);
+                        if (B_MN) {
 #pragma unroll
-                        for (int j = 0; j < BN / 64; ++j) tma_2d(b + j * kTK * 128, &mb, n0 + 64 * j, k * kTK, &full[st]);
-                    } else
-                        tma_2d(b, &mb, k * kTK, n0, &full[st]);
+                            for (int j = 0; j < G::b_rows / 64; ++j)
+                                tma_2d<PAIR>(b + j * kTK * 128, &mb, n0 + 64 * j, k * kTK, bar);
+                        } else
+                            tma_2d<PAIR>(b, &mb, k * kTK, n0, bar);
+                    }
+                    if (++st == G::ST) st = 0, ph ^= 1, lap = true;
                 }
             }
-            // every issued copy lands before the CTA may leave
-            for (int64_t j = i > G::ST ? i - G::ST : 0; j < i; ++j)
-                u_mb_wait(&full[j % G::ST], (int)(j / G::ST) & 1, nullptr);
-        } else if (w == 1 && lane == 0) {  // MMA issuer
+            // every issued copy lands before the CTA may leave (and has been read:
+            // the pair's second CTA sees its copies' arrival only in that)
+            for (int j = 0; j < G::ST; ++j) {
+                if (!lap && st == 0) break;
+                if (--st < 0) st = G::ST - 1, ph ^= 1, lap = false;
+                u_mb_wait(rank ? &empty[st] : &full[st], ph, nullptr);
+            }
+        } else if (w == 1 && rank == 0) {  // MMA issuer
             const uint32_t idesc = (1u << 4) | (g.bf16 ? 1u << 7 | 1u << 10 : 0u) | (A_MN ? 1u << 15 : 0u) |
-                                   (B_MN ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) | (8u << 24);
+                                   (B_MN ? 1u << 16 : 0u) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(kTM * CG >> 4) << 24);
             const uint64_t da0 = sw128_desc(u_saddr(sm), A_MN), db0 = sw128_desc(u_saddr(sm) + kABytes, B_MN);
             constexpr uint32_t a_step = (A_MN ? 16 * 128 : 32) >> 4, b_step = (B_MN ? 16 * 128 : 32) >> 4;
-            int64_t i = 0;
+            int st = 0, ph = 0;
             unsigned u = 0;
             bool ok = true;
-            for (int it = blockIdx.x; it < items && ok; it += gridDim.x) {
+            for (int it = first; it < items && ok; it += stride) {
                 const int s = it / tiles;
                 const int ks = (int)((int64_t)g.nk * (s + 1) / g.S) - (int)((int64_t)g.nk * s / g.S);
-                for (int c0 = 0; c0 < ks && ok; c0 += kChain, ++u) {
-                    if (u >= 2 && !u_mb_wait(&acc_empty[u & 1], ((u >> 1) - 1) & 1, stall)) {
+                for (int c0 = 0; c0 < ks && ok; c0 += g.chain, ++u) {
+                    if (u >= 2 && !__all_sync(kFull, u_mb_wait(&acc_empty[u & 1], ((u >> 1) - 1) & 1, stall))) {
                         *stall = kErrStall;
                         ok = false;
                         break;
                     }
                     u_fence_after();
-                    const int c1 = c0 + kChain < ks ? c0 + kChain : ks;
-                    for (int k = c0; k < c1; ++k, ++i) {
-                        const int st = (int)(i % G::ST);
-                        if (!u_mb_wait(&full[st], (int)(i / G::ST) & 1, stall)) {
+                    const int c1 = c0 + g.chain < ks ? c0 + g.chain : ks;
+                    for (int k = c0; k < c1; ++k) {
+                        if (!__all_sync(kFull, u_mb_wait(&full[st], ph, stall))) {
                             *stall = kErrStall;
                             ok = false;
                             break;
                         }
                         u_fence_after();
                         const uint32_t at = (uint32_t)(st * G::stage) >> 4;
+                        if (elect()) {
 #pragma unroll
-                        for (int kk = 0; kk < kTK / 16; ++kk)
-                            u_mma(tmem + (u & 1) * BN, da0 + at + kk * a_step, db0 + at + kk * b_step, idesc,
-                                  k > c0 || kk > 0);
-                        u_commit(&empty[st]);
+                            for (int kk = 0; kk < kTK / 16; ++kk)
+                                mma<PAIR>(tmem + (u & 1) * BN, da0 + at + kk * a_step, db0 + at + kk * b_step, idesc,
+                                          k > c0 || kk > 0);
+                            commit<PAIR>(&empty[st]);
+                            if (k + 1 == c1) commit<PAIR>(&acc_full[u & 1]);
+                        }
+                        if (++st == G::ST) st = 0, ph ^= 1;
                     }
-                    if (ok) u_commit(&acc_full[u & 1]);
                 }
             }
-            u_commit(done);  // after every MMA this thread issued
+            if (elect()) commit<PAIR>(done);  // after every MMA this warp issued
             u_mb_wait(done, 0, nullptr);
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int q = w & 3, h = (w - 4) >> 2;
         constexpr int HC = BN / 2;  // columns of a warp
         float* so = stage_out + (w - 4) * 1024;
         const uint32_t t0 = tmem + ((uint32_t)(32 * q) << 16) + h * HC;
         unsigned u = 0;
         bool ok = true;
-        for (int it = blockIdx.x; it < items; it += gridDim.x) {
-            const int tile = it % tiles, s = it / tiles, m0 = tile % g.mt * kTM + 32 * q, n0 = tile / g.mt * BN + h * HC;
+        for (int it = first; it < items; it += stride) {
+            const int tile = it % tiles, s = it / tiles;
+            const int m0 = (tile % g.mt * CG + rank) * kTM + 32 * q, n0 = tile / g.mt * BN + h * HC;
             const int ks = (int)((int64_t)g.nk * (s + 1) / g.S) - (int)((int64_t)g.nk * s / g.S);
             float acc[HC];
 #pragma unroll
             for (int i = 0; i < HC; ++i) acc[i] = 0.f;
-            for (int c0 = 0; c0 < ks; c0 += kChain, ++u) {
+            for (int c0 = 0; c0 < ks; c0 += g.chain, ++u) {
                 if (ok && !u_mb_wait(&acc_full[u & 1], (u >> 1) & 1, stall)) {
                     *stall = kErrStall;
                     ok = false;
@@ -394,7 +515,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 }
                 u_fence_before();
                 __syncwarp();
-                if (lane == 0) u_mb_arrive(&acc_empty[u & 1]);
+                if (lane == 0) {
+                    if (PAIR) arrive_cluster(leader_addr(&acc_empty[u & 1]));
+                    else u_mb_arrive(&acc_empty[u & 1]);
+                }
             }
             if (!ok) {
 #pragma unroll
@@ -402,27 +526,43 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             }
             if (m0 >= g.M) continue;
             // 32 x 32 blocks through shared memory, so that four lanes write 32
-            // neighbouring columns of a row: 16-byte pieces, swizzled by the row
-#pragma unroll
-            for (int c = 0; c < HC; c += 32) {
-                if (n0 + c >= g.N) break;
-                float4* s4 = reinterpret_cast<float4*>(so);
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    s4[lane * 8 + (j ^ (lane & 7))] =
-                        make_float4(acc[c + 4 * j], acc[c + 4 * j + 1], acc[c + 4 * j + 2], acc[c + 4 * j + 3]);
-                __syncwarp();
-                const int col = n0 + c + 8 * (lane & 3);
+            // neighbouring columns of a row: 16-byte pieces, swizzled by the row.
+            // One body for all blocks: unrolled, its instructions came from memory
+            // for every tile (10000 cycles a tile of 128 x 256).
+            float4* s4 = reinterpret_cast<float4*>(so);
 #pragma unroll 1
-                for (int i = 0; i < 4; ++i) {
-                    const int lr = 8 * i + (lane >> 2), row = m0 + lr, ch = 2 * (lane & 3);
-                    const float4 a = s4[lr * 8 + (ch ^ (lr & 7))], b = s4[lr * 8 + ((ch + 1) ^ (lr & 7))];
-                    float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-                    if (row < g.M && col < g.N) {
+            for (int c = 0; c < HC && n0 + c < g.N; c += 32) {
+#pragma unroll
+                for (int b = 0; b < HC; b += 32)
+                    if (b == c) {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            s4[lane * 8 + (j ^ (lane & 7))] =
+                                make_float4(acc[b + 4 * j], acc[b + 4 * j + 1], acc[b + 4 * j + 2], acc[b + 4 * j + 3]);
+                    }
+                __syncwarp();
+                const int col = n0 + c + 8 * (lane & 3), ch = 2 * (lane & 3), row = m0 + (lane >> 2);
+                auto piece = [&](int i, float (&v)[8]) {
+                    const int lr = 8 * i + (lane >> 2);
+                    const float4 x = s4[lr * 8 + (ch ^ (lr & 7))], y = s4[lr * 8 + ((ch + 1) ^ (lr & 7))];
+                    v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
+                    v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+                };
+                if (g.S == 1 && g.e.act == EE_ACT_NONE && g.vec && m0 + 32 <= g.M && n0 + c + 32 <= g.N) {
+                    float v[4][8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) piece(i, v[i]);
+                    emit8x4(g.e, row, col, v);
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < 4; ++i) {
+                        float v[8];
+                        piece(i, v);
+                        if (row + 8 * i >= g.M || col >= g.N) continue;
                         if (g.S > 1)
-                            store8(g.part + ((int64_t)s * g.M + row) * g.ldp + col, EE_FP32, 8, true, v);
+                            store8(g.part + ((int64_t)s * g.M + row + 8 * i) * g.ldp + col, EE_FP32, 8, true, v);
                         else
-                            emit8(g.e, row, col, g.N - col, v);
+                            emit8(g.e, row + 8 * i, col, g.N - col, v);
                     }
                 }
                 __syncwarp();
@@ -432,8 +572,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     __syncwarp();
     u_fence_before();
     __syncthreads();
-    if (w == 2)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(G::tmem) : "memory");
+    if (PAIR) cluster_barrier();  // the first CTA's MMAs read the second's operands
+    if (w == 2) {
+        if constexpr (PAIR)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(G::tmem) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(G::tmem) : "memory");
+    }
 }
 
 // The splits' partial sums in split order, then the epilogue; 8 columns per
@@ -577,39 +722,70 @@ bool make_map(CUtensorMap* map, const Mat& m, int type, int box_rows) {
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Tile width and k splits: the pair with the least estimated time.  A stage
-// costs its MMAs (2 BN cycles) or, for narrow tiles, about 260 cycles of copy;
-// a wave of items fills and drains the ring once (1500 cycles); splits write
-// and read their partial sums (about 2400 bytes a cycle over the whole GPU) and
-// take another launch (4000 cycles).
+// Tile shape and k splits: the choice with the least estimated time, in SM
+// cycles.  A stage costs its MMAs (2 BN) or the copy of its operands, which
+// arrive at about 51 bytes a cycle per SM (measured: 640 for the 32 KB of a pair
+// with BN = 256, 900 for the 48 KB of a CTA by itself); set-up and the first copy
+// take 4200, the last tile's write 12 per column; splits write and read their
+// partial sums (about 2400 bytes a cycle over the whole GPU) and take another
+// launch (4000).
 struct Tiling {
     int bn, S;
+    bool pair;
 };
 Tiling tiling(int64_t M, int64_t N, int nk, int n_sm) {
-    Tiling best{64, 1};
+    Tiling best{64, 1, false};
     double best_t = 1e30;
-    for (int bn = 64; bn <= 256; bn *= 2)
-        for (int S = 1; S <= 32 && S <= (nk + 1) / 2; ++S) {
-            const int64_t items = (M + kTM - 1) / kTM * ((N + bn - 1) / bn) * S;
-            const double waves = (double)((items + n_sm - 1) / n_sm);
-            double t = waves * ((nk + S - 1) / S * std::max(2.0 * bn, 260.0) + 600) + 1500;
-            if (S > 1) t += 4000 + 8.0 * (double)S * M * N / 2400;
-            if (t < best_t) best_t = t, best = {bn, S};
-        }
+    for (int pair = 0; pair < 2; ++pair)
+        for (int bn = pair ? 128 : 64; bn <= 256; bn *= 2)
+            for (int S = 1; S <= 32 && S <= (nk + 1) / 2; ++S) {
+                const int tm = kTM << pair, units = n_sm >> pair;
+                const int64_t items = (M + tm - 1) / tm * ((N + bn - 1) / bn) * S;
+                const double waves = (double)((items + units - 1) / units);
+                const double stage = std::max(2.0 * bn, (kTM + (bn >> pair)) * 128 / 51.0);
+                double t = 4200 + waves * ((nk + S - 1) / S) * stage + 12.0 * bn;
+                if (S > 1) t += 4000 + 8.0 * (double)S * M * N / 2400;
+                if (t < best_t) best_t = t, best = {bn, S, pair != 0};
+            }
     return best;
 }
 
-template <int BN, bool A_MN, bool B_MN>
+template <int BN, bool PAIR, bool A_MN, bool B_MN>
 int launch_gemm(const Ctx& c, const Mat& A, const Mat& B, const GemmArgs& g) {
+    using G = GShape<BN, PAIR>;
     CUtensorMap ma, mb;
-    if (!make_map(&ma, A, c.type, A_MN ? kTK : kTM) || !make_map(&mb, B, c.type, B_MN ? kTK : BN))
+    if (!make_map(&ma, A, c.type, A_MN ? kTK : kTM) || !make_map(&mb, B, c.type, B_MN ? kTK : G::b_rows))
         return fail(EE_ECUDA, "cuTensorMapEncodeTiled failed");
-    auto* k = k_gemm<BN, A_MN, B_MN>;
-    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GShape<BN>::smem);
+    auto* k = k_gemm<BN, PAIR, A_MN, B_MN>;
+    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)G::smem);
     if (e != cudaSuccess) return cuda_status(e);
+    cudaLaunchConfig_t cfg{};
+    cfg.blockDim = dim3(kGemmThreads);
+    cfg.dynamicSmemBytes = G::smem;
+    cfg.stream = c.s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = G::CG;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = PAIR ? 1 : 0;
+    int units = c.n_sm;
+    if (PAIR) {
+        // pairs that run at the same time: a cluster lies within a group of SMs, so
+        // that there may be fewer than half the SMs' number (the same for every call)
+        static std::atomic<int> pairs{0};
+        units = pairs.load(std::memory_order_relaxed);
+        if (!units) {
+            cfg.gridDim = dim3(2);
+            e = cudaOccupancyMaxActiveClusters(&units, k, &cfg);
+            if (e != cudaSuccess) return cuda_status(e);
+            if (units < 1) return fail(EE_ECUDA, "no room for a pair of CTAs");
+            pairs.store(units, std::memory_order_relaxed);
+        }
+    }
     const int64_t items = (int64_t)g.mt * g.nt * g.S;
-    k<<<(unsigned)std::min<int64_t>(items, c.n_sm), kGemmThreads, GShape<BN>::smem, c.s>>>(ma, mb, g);
-    return cuda_status(cudaGetLastError());
+    cfg.gridDim = dim3((unsigned)(std::min<int64_t>(items, units) * G::CG));
+    return cuda_status(cudaLaunchKernelEx(&cfg, k, ma, mb, g));
 }
 
 // D = A B^T.  A_MN / B_MN: the operand is stored with k as its rows.
@@ -625,8 +801,11 @@ int gemm(Ctx& c, Mat A, Mat B, const Epilogue& e) {
     g.N = (int)N;
     g.nk = (int)((K + kTK - 1) / kTK);
     g.bf16 = c.type == EE_BF16;
+    g.chain = e.out_type == EE_FP32 ? 8 : 32;
+    g.vec = e.vec_all();
     const Tiling t = tiling(M, N, g.nk, c.n_sm);
-    g.mt = (int)((M + kTM - 1) / kTM);
+    const int tm = t.pair ? 2 * kTM : kTM;
+    g.mt = (int)((M + tm - 1) / tm);
     g.nt = (int)((N + t.bn - 1) / t.bn);
     g.S = t.S;
     if ((int64_t)g.mt * g.nt * g.S > 0x7fffffff) return fail(EE_EINVAL, "too many rows");
@@ -634,9 +813,12 @@ int gemm(Ctx& c, Mat A, Mat B, const Epilogue& e) {
     if (t.S > 1) g.part = (float*)c.mem.take(4 * (size_t)t.S * M * g.ldp);
     g.e = e;
     if (c.dry) return EE_OK;
-    rc = t.bn == 256 ? launch_gemm<256, A_MN, B_MN>(c, A, B, g)
-         : t.bn == 128 ? launch_gemm<128, A_MN, B_MN>(c, A, B, g)
-                       : launch_gemm<64, A_MN, B_MN>(c, A, B, g);
+    if (t.pair)
+        rc = t.bn == 256 ? launch_gemm<256, true, A_MN, B_MN>(c, A, B, g) : launch_gemm<128, true, A_MN, B_MN>(c, A, B, g);
+    else
+        rc = t.bn == 256   ? launch_gemm<256, false, A_MN, B_MN>(c, A, B, g)
+             : t.bn == 128 ? launch_gemm<128, false, A_MN, B_MN>(c, A, B, g)
+                           : launch_gemm<64, false, A_MN, B_MN>(c, A, B, g);
     if (rc != EE_OK || t.S == 1) return rc;
     k_join<<<n_blocks(M * (g.ldp / 8), 256), 256, 0, c.s>>>(g);
     return cuda_status(cudaGetLastError());

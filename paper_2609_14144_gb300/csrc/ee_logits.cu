@@ -4,11 +4,9 @@
 // (ee_distill_topk, ee_distill_topk_backward).
 //
 // All of them are bound by reading (and, for the gradient, writing) the logits
-// once.  A row is streamed by one CTA, or by a cluster of up to 8 CTAs when
-// there are few rows, each thread with a running maximum m and the sum of
-// 2^((x - m) c), c = log2(e) / T, in 32 bits; the threads' pairs join in the
-// warp, the CTA and the cluster.  x - m is formed before the product with c, so
-// that rows masked with the type's lowest value do not overflow.
+// once.  A row is streamed by one CTA or by a cluster of up to 8 CTAs, each thread
+// with a running maximum m and the sum of 2^((x - m) c), c = log2(e) / T, in 32
+// bits; the threads' pairs join in the warp, the CTA and the cluster.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -19,21 +17,30 @@
 #include <algorithm>
 
 #include "ee_internal.h"
+#include "ee_umma.cuh"
 
 namespace cg = cooperative_groups;
 
 namespace ee {
 namespace {
 
-constexpr int kLT = 256;      // threads per CTA
-constexpr int kLU = 4;        // 16-byte vectors per thread and batch
-constexpr int kCand = 2048;   // candidates a CTA collects for the best tokens
+constexpr int kBT = 256;       // threads per CTA of the backward pass
+constexpr int kLU = 4;         // its 16-byte vectors per thread and batch
+constexpr int kCand = 1024;    // candidates a CTA collects for the best tokens
+constexpr int kEnough = 320;   // as many are ranked against each other
+constexpr int kMaxGroups = 16; // groups of vectors per thread whose maxima are kept
+constexpr int kMaxHits = 512;
 constexpr int kMaxList = EE_MAX_TOP;
 constexpr int kMaxCluster = 8;
-constexpr int kMaxBits = (EE_MAX_VOCAB / kMaxCluster) / 8 + 256;  // shared bytes of a slice's listed bits
+constexpr int kMaxSlice = EE_MAX_VOCAB / kMaxCluster;  // elements of a row per CTA
+constexpr int64_t kL2Rows = 50 << 20;  // bytes of rows in flight that L2 keeps (of its 129 MB)
 constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kInf = __builtin_huge_valf();
+constexpr float kNan = __builtin_nanf("");
 constexpr unsigned kFull = 0xffffffffu;
+
+// Words of a slice's listed bits.
+__host__ __device__ inline int slice_words(int vocab, int E, int cs) { return (((vocab / E + 2) / cs + 1) * E + 31) / 32 + 1; }
 
 __device__ __forceinline__ float ex2(float t) {
     float r;
@@ -73,8 +80,25 @@ struct El<EE_BF16> {
         const __nv_bfloat162 a = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
         return max_nan(__low2float(a), __high2float(a));
     }
+    // Elements no lower than a value whose power is 0 beside any maximum that is not wide.
+    static __device__ __forceinline__ uint4 floor(uint4 v) {
+        __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+        const __nv_bfloat162 lo = __float2bfloat162_rn(-1e30f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __hmax2_nan(h[i], lo);
+        return v;
+    }
     static __device__ __forceinline__ float one(T v) { return __uint_as_float((uint32_t)v << 16); }
     static __device__ __forceinline__ T put(float f) { return __bfloat16_as_ushort(__float2bfloat16_rn(f)); }
+    static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+        uint4 r;
+        __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        return r;
+    }
+    // (powers below 2^-126 become 0: a 16-bit gradient loses at most its subnormals)
+    static __device__ __forceinline__ float power(float t) { return ex2(t); }
 };
 template <>
 struct El<EE_FP16> {
@@ -95,8 +119,23 @@ struct El<EE_FP16> {
         const __half2 a = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
         return max_nan(__low2float(a), __high2float(a));
     }
+    static __device__ __forceinline__ uint4 floor(uint4 v) {
+        __half2* h = reinterpret_cast<__half2*>(&v);
+        const __half2 lo = __float2half2_rn(-65504.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __hmax2_nan(h[i], lo);
+        return v;
+    }
     static __device__ __forceinline__ float one(T v) { return __half2float(__ushort_as_half(v)); }
     static __device__ __forceinline__ T put(float f) { return __half_as_ushort(__float2half_rn(f)); }
+    static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+        uint4 r;
+        __half2* h = reinterpret_cast<__half2*>(&r);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+        return r;
+    }
+    static __device__ __forceinline__ float power(float t) { return ex2(t); }
 };
 template <>
 struct El<EE_FP32> {
@@ -113,8 +152,18 @@ struct El<EE_FP32> {
         return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)),
                        max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
     }
+    static __device__ __forceinline__ uint4 floor(uint4 v) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(max_nan(__uint_as_float(w[i]), -1e30f));
+        return v;
+    }
     static __device__ __forceinline__ float one(T v) { return __uint_as_float(v); }
     static __device__ __forceinline__ T put(float f) { return __float_as_uint(f); }
+    static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+        return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+    }
+    static __device__ __forceinline__ float power(float t) { return ex2_full(t); }
 };
 
 // A row as 16-byte vectors: vector v holds elements [v E - mis, v E - mis + E)
@@ -150,57 +199,323 @@ struct Row {
 };
 
 // ---------------------------------------------------------------- running softmax
-// m: largest value so far (-inf: none); s: sum of 2^((x - m) c); a: sum of
-// t 2^t, t = (x - m) c, from which the entropy follows.
+// Powers are taken relative to r = m c rounded to 32 bits, as one fused
+// multiply-add per element, t = x c - r, two elements at a time.  Every use of
+// (m, r) rounds alike, so that r's rounding shifts all of a row's powers by the
+// same factor, which log_sum() takes back in the row's result.  Rows whose maximum
+// is too large for that ("wide": r near overflow, or m so low that the stand-in
+// for -inf would count) form x - m first.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 v, float& lo, float& hi) {
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+template <int DT>
+__device__ __forceinline__ bool wide(float m, float c) {
+    const float r = __fmul_rn(m, c);
+    return !(r < 1e37f && r > -1e37f && m > (DT == EE_FP16 ? -3e4f : -1e28f)) && m != -kInf;
+}
+// The reference of maximum m (0 while there is none).
+__device__ __forceinline__ float ref_of(float m, float c) { return m == -kInf ? 0.f : __fmul_rn(m, c); }
+template <int DT>
+__device__ __forceinline__ float exponent(float x, float m, float c) {
+    return wide<DT>(m, c) ? (x - m) * c : fmaf(x, c, -ref_of(m, c));
+}
+// How far the powers relative to m1 lie below those relative to m2.
+template <int DT>
+__device__ __forceinline__ float shift_of(float m1, float m2, float c) {
+    return wide<DT>(m1, c) || wide<DT>(m2, c) ? (m1 - m2) * c : ref_of(m1, c) - ref_of(m2, c);
+}
+// m: largest value so far (-inf: none); s: sum of 2^t; a: sum of t 2^t, from
+// which the entropy follows.
 struct Run {
     float m, s, a;
 };
 // Rescale to the larger maximum m2.
+template <int DT>
 __device__ __forceinline__ void run_to(Run& r, float m2, float c) {
-    const float d = (r.m - m2) * c, f = ex2(d);
-    const bool none = r.m == -kInf || f == 0.f;  // (0 times an infinite d would be NaN)
-    r.a = none ? 0.f : f * (r.a + d * r.s);
-    r.s = none && r.s == r.s ? 0.f : f * r.s;
+    if (r.m != -kInf) {  // (before the first value s is 0, or NaN if one was seen)
+        const float d = shift_of<DT>(r.m, m2, c), f = ex2(d);
+        r.a = f == 0.f ? 0.f : f * (r.a + d * r.s);  // (0 times an infinite d would be NaN)
+        r.s = f * r.s;
+    }
     r.m = m2;
 }
-__device__ __forceinline__ void run_join(Run& r, Run o, float c) {
-    if (o.m > r.m) {
-        const Run t = r;
-        r = o;
-        o = t;
+// A thread's running softmax: the sums in pairs.
+template <int DT, bool ENT>
+struct Acc {
+    float m = -kInf, r = 0.f;
+    bool far = false;  // wide(m)
+    f32x2 s = 0, a = 0;
+    __device__ __forceinline__ Run get() const {
+        float s0, s1, a0, a1;
+        unpack2(s, s0, s1);
+        unpack2(a, a0, a1);
+        return Run{m, s0 + s1, a0 + a1};
     }
-    if (o.m == -kInf) {  // nothing in o, but a NaN stays one
-        r.s += o.s;
-        return;
+    __device__ __noinline__ static Run moved(Run q, float vm, float c) {
+        run_to<DT>(q, vm, c);
+        return q;
     }
-    run_to(o, r.m, c);
-    r.s += o.s;
-    r.a += o.a;
+    // Adds a vector whose largest element is vm (NaN if it holds one).
+    __device__ __forceinline__ void add(uint4 v, float vm, float c) {
+        constexpr int E = El<DT>::E;
+        if (vm > m) {
+            const Run q = moved(get(), vm, c);
+            m = q.m;
+            s = pack2(q.s, 0.f);
+            a = pack2(q.a, 0.f);
+            r = ref_of(m, c);
+            far = wide<DT>(m, c);
+        }
+        float x[E];
+        if (far) {
+            El<DT>::unpack(v, x);
+            float p = 0.f, q = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float t = (x[e] - m) * c, w = ex2(t);
+                p += w;
+                q = fmaf(w, fmaxf(t, -1e6f), q);
+            }
+            s = add2(s, pack2(p, 0.f));
+            if (ENT) a = add2(a, pack2(q, 0.f));
+            return;
+        }
+        if (ENT) v = El<DT>::floor(v);  // -inf times its power 0 would be NaN
+        El<DT>::unpack(v, x);
+        const f32x2 c2 = pack2(c, c), r2 = pack2(-r, -r);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+            const f32x2 t = fma2(pack2(x[e], x[e + 1]), c2, r2);
+            float t0, t1;
+            unpack2(t, t0, t1);
+            const f32x2 p = pack2(ex2(t0), ex2(t1));
+            s = add2(s, p);
+            if (ENT) a = fma2(p, t, a);
+        }
+    }
+};
+// ---------------------------------------------------------------- streaming
+// A cluster of `cs` CTAs takes rows one after the other, each CTA a slice of the
+// row's vectors.  One warp of a CTA keeps a ring of shared-memory stages filled
+// by bulk copies, ahead through the passes and rows that follow, so that HBM
+// stays busy while the others reduce, select or write; twelve warps consume; one
+// more prepares the next row's list where there is one.  Two CTAs fit an SM.
+// Loading through registers instead (four vectors per thread, one batch ahead)
+// reached 4.7 TB/s in the stream and nothing between: 219 us where a pass over
+// 2048 x 151936 bf16 takes 92 us of reading.
+constexpr int kNT = 384;                 // consuming threads
+constexpr int kWarps = kNT / 32;
+constexpr int kThreads = kNT + 64;
+constexpr int kPer = 2;                  // vectors per thread and chunk
+constexpr int kChunk = kNT * kPer;       // vectors per stage: 12 KB
+constexpr int kStages = 6;
+constexpr int kRingBytes = kStages * kChunk * 16;
+
+__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 384;" ::: "memory"); }
+static_assert(kNT == 384, "consumers_sync");
+
+// m: largest value so far (-inf: none); s: sum of 2^t; a: sum of t 2^t.
+struct Link {
+    uint64_t full[kStages], empty[kStages], list_full[2], list_empty[2], exchange, joined;
+    float4 peer[2][kMaxCluster];
+    float4 warp[2][kWarps];
+    int stall;  // a wait ran out: no further wait, results from here on are NaN
+};
+
+__device__ __forceinline__ bool try_wait_cluster(uint64_t* b, int parity) {
+    uint32_t ok;
+    asm volatile(
+        "{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+        : "=r"(ok)
+        : "r"(u_saddr(b)), "r"(parity)
+        : "memory");
+    return ok != 0;
 }
-__device__ __forceinline__ Run run_shfl(const Run& r, int off) {
-    return Run{__shfl_xor_sync(kFull, r.m, off), __shfl_xor_sync(kFull, r.s, off), __shfl_xor_sync(kFull, r.a, off)};
+// Waits for the phase of the given parity, at most about 2 s.
+__device__ __noinline__ bool wait_slow(Link& l, uint64_t* b, int parity) {
+    volatile int* stall = &l.stall;
+    const long long t0 = clock64();
+    for (unsigned it = 1;; ++it) {
+        if (try_wait_cluster(b, parity)) return true;
+        if ((it & 255) == 0 && (*stall || clock64() - t0 > kUWaitCycles)) break;
+    }
+    *stall = 1;
+    return false;
+}
+__device__ __forceinline__ bool wait(Link& l, uint64_t* b, int parity) {
+    return try_wait_cluster(b, parity) || wait_slow(l, b, parity);
+}
+__device__ __forceinline__ void expect_tx(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(u_saddr(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_copy(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(u_saddr(dst)),
+                 "l"(src), "r"(bytes), "r"(u_saddr(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void arrive_at(uint64_t* bar, int rank) {
+    uint32_t p;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"(u_saddr(bar)), "r"(rank));
+    asm volatile("fence.acq_rel.cluster;" ::: "memory");
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(p) : "memory");
 }
 
-// The CTA's joined state, then the cluster's; every thread returns it.
-struct RunShared {
-    Run warp[kLT / 32];
-    Run cta;
-};
-__device__ Run run_reduce(Run r, RunShared& sh, float c, int cs) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) run_join(r, run_shfl(r, o), c);
-    if ((threadIdx.x & 31) == 0) sh.warp[threadIdx.x >> 5] = r;
+__device__ void link_init(Link& l, int cs) {
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            u_mb_init(&l.full[i], 1);
+            u_mb_init(&l.empty[i], kWarps);
+        }
+        for (int i = 0; i < 2; ++i) {
+            u_mb_init(&l.list_full[i], 1);
+            u_mb_init(&l.list_empty[i], kWarps);
+        }
+        u_mb_init(&l.exchange, cs);
+        u_mb_init(&l.joined, cs > 1 ? cs - 1 : 1);
+        l.stall = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
     __syncthreads();
-    r = sh.warp[0];
-    for (int i = 1; i < kLT / 32; ++i) run_join(r, sh.warp[i], c);
-    if (cs > 1) {
-        cg::cluster_group cl = cg::this_cluster();
-        if (threadIdx.x == 0) sh.cta = r;
-        cl.sync();
-        r = *cl.map_shared_rank(&sh.cta, 0);
-        for (int i = 1; i < cs; ++i) run_join(r, *cl.map_shared_rank(&sh.cta, i), c);
+    if (cs > 1) cg::this_cluster().sync();
+}
+
+// The ring's position; every user steps through the same sequence of stages.
+struct Turn {
+    int st = 0, ph = 0;
+    __device__ __forceinline__ void step() {
+        if (++st == kStages) st = 0, ph ^= 1;
+    }
+};
+
+// A CTA's slice of a row.
+template <int DT>
+struct Slice {
+    Row<DT> row;
+    int v0, v1, f0, f1;  // its vectors; those of the row that lie wholly in it
+    __device__ Slice(const void* p, int64_t ld, int64_t r, int vocab, int rank, int cs) : row(p, ld, r, vocab) {
+        v0 = (int)((int64_t)row.nv * rank / cs);
+        v1 = (int)((int64_t)row.nv * (rank + 1) / cs);
+        f0 = row.mis ? 1 : 0;
+        f1 = (int)(((int64_t)row.V + row.mis) / El<DT>::E);
+    }
+    __device__ int chunks() const { return (v1 - v0 + kChunk - 1) / kChunk; }
+};
+
+// Fills the ring with one pass over the slice (one thread).  `n` counts the
+// stages filled so far.
+template <int DT>
+__device__ bool feed(const Slice<DT>& s, uint4* ring, Link& l, Turn& t, int64_t& n) {
+    for (int vb = s.v0; vb < s.v1; vb += kChunk, t.step(), ++n) {
+        if (n >= kStages && !wait(l, &l.empty[t.st], t.ph ^ 1)) return false;
+        const int lo = max(vb, s.f0), hi = min(min(vb + kChunk, s.v1), s.f1);
+        const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) * 16 : 0;
+        expect_tx(&l.full[t.st], bytes);
+        if (bytes)
+            bulk_copy(ring + t.st * kChunk + (lo - vb), s.row.p + ((int64_t)lo * El<DT>::E - s.row.mis), bytes, &l.full[t.st]);
+    }
+    return true;
+}
+// Every copy lands before the CTA may leave.
+__device__ void drain(Link& l, Turn t, int64_t n) {
+    const long long t0 = clock64();
+    for (int i = 0; i < kStages && i < n; ++i) {
+        // the stage filled i + 1 steps ago
+        if (--t.st < 0) t.st = kStages - 1, t.ph ^= 1;
+        while (!try_wait_cluster(&l.full[t.st], t.ph))
+            if (clock64() - t0 > kUWaitCycles) return;
+    }
+}
+
+// This thread's vectors of the chunk at vb, and the stage's release.
+template <int DT>
+__device__ __forceinline__ bool fetch(const Slice<DT>& s, const uint4* ring, Link& l, Turn& t, int vb, uint4 (&cur)[kPer]) {
+    const bool ok = wait(l, &l.full[t.st], t.ph);
+    const uint4* st = ring + t.st * kChunk + threadIdx.x;
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+        const int v = vb + threadIdx.x + u * kNT;
+        if (v >= s.f0 && v < s.f1 && v < s.v1) cur[u] = st[u * kNT];
+        else if (v < s.v1) cur[u] = s.row.load_edge((int64_t)v * El<DT>::E - s.row.mis);
+        else cur[u] = make_uint4(El<DT>::ninf, El<DT>::ninf, El<DT>::ninf, El<DT>::ninf);
+    }
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) u_mb_arrive(&l.empty[t.st]);
+    t.step();
+    return ok;
+}
+
+// The row's joined softmax from the threads' and, in a cluster, the CTAs'.
+// turn: the row's number; *cta: the CTA's own.
+template <int DT>
+__device__ __forceinline__ Run join_warps(const float4* w, int n, float c) {
+    float m = -kInf;
+    for (int i = 0; i < n; ++i) m = fmaxf(m, w[i].x);
+    Run r{m, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        Run o{w[i].x, w[i].y, w[i].z};
+        if (o.m != m) run_to<DT>(o, m, c);
+        r.s += o.s;
+        r.a += o.a;
     }
     return r;
+}
+template <int DT>
+__device__ __forceinline__ Run row_reduce(Run r, Link& l, float c, int turn, int rank, int cs, Run* cta) {
+    float m = r.m;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
+    if (r.m != m) run_to<DT>(r, m, c);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        r.s += __shfl_xor_sync(kFull, r.s, o);
+        r.a += __shfl_xor_sync(kFull, r.a, o);
+    }
+    const int p = turn & 1;
+    if ((threadIdx.x & 31) == 0) l.warp[p][threadIdx.x >> 5] = make_float4(m, r.s, r.a, 0.f);
+    consumers_sync();
+    r = join_warps<DT>(l.warp[p], kWarps, c);
+    *cta = r;
+    if (cs > 1) {
+        if (threadIdx.x < cs) {
+            cg::cluster_group cl = cg::this_cluster();
+            *cl.map_shared_rank(&l.peer[p][rank], threadIdx.x) = make_float4(r.m, r.s, r.a, 0.f);
+            arrive_at(&l.exchange, threadIdx.x);
+        }
+        const bool ok = wait(l, &l.exchange, p);
+        r = join_warps<DT>(l.peer[p], cs, c);
+        if (!ok) r.s = kNan;
+    }
+    return r;
+}
+
+// ln of the sum of exp((x - m) / T), from the sum of powers relative to r.
+template <int DT>
+__device__ __forceinline__ float log_sum(float s, float m, float c) {
+    const float lns = logf(s);
+    return m == -kInf || wide<DT>(m, c) ? lns : lns - fmaf(m, c, -ref_of(m, c)) * kLn2;
 }
 
 // ---------------------------------------------------------------- best tokens
@@ -222,53 +537,52 @@ __device__ __forceinline__ unsigned long long key_of(float x, int idx) {
 struct TopShared {
     unsigned long long keys[kCand];
     unsigned long long best[kMaxList];
-    unsigned long long surv[2 * kMaxList + 128];
+    unsigned long long surv[kEnough];
+    unsigned long long join[(kMaxCluster - 1) * kMaxList];  // the first CTA's: the others' best
+    uint16_t group[kMaxGroups * kNT];  // upper half of the order of each group's maximum
     unsigned hist[256];
+    int list[kMaxHits];  // groups that may hold one of the best
+    int join_n[kMaxCluster];
+    int n_hits;
     int n;         // candidates pushed (may pass kCand: the surplus was dropped)
     int n_surv;
-    int sum[3];    // rotating counters of block_sum, zero between uses
+    int2 sum[3];   // rotating counters of block_sum, zero between uses
     unsigned long long prefix;
     int done;
 };
 
-// Sum over the CTA with one barrier: a slot is cleared two calls before it is
-// used again.
-__device__ __forceinline__ int block_sum(int v, TopShared& sh, int& turn) {
-    v = __reduce_add_sync(kFull, v);
+// Two sums over the consumers with one barrier: a slot is cleared two calls
+// before it is used again.
+__device__ __forceinline__ int2 block_sum(int a, int b, TopShared& sh, int& turn) {
+    a = __reduce_add_sync(kFull, a);
+    b = __reduce_add_sync(kFull, b);
     const int slot = turn % 3;
-    if ((threadIdx.x & 31) == 0 && v) atomicAdd(&sh.sum[slot], v);
-    __syncthreads();
-    const int r = sh.sum[slot];
-    if (threadIdx.x == 0) sh.sum[(turn + 2) % 3] = 0;
+    if ((threadIdx.x & 31) == 0) {
+        if (a) atomicAdd(&sh.sum[slot].x, a);
+        if (b) atomicAdd(&sh.sum[slot].y, b);
+    }
+    consumers_sync();
+    const int2 r = sh.sum[slot];
+    if (threadIdx.x == 0) sh.sum[(turn + 2) % 3] = make_int2(0, 0);
     ++turn;
     return r;
 }
 
-// Of the n keys, the largest prefix (over the bits from 63 down to `last`) that
-// at least `want` keys reach; stops early once at most `enough` do.  Every
-// thread returns it.
-__device__ unsigned long long key_prefix(const unsigned long long* keys, int n, int want, int enough, int last,
-                                         TopShared& sh, int& turn) {
+// Of the n keys, the largest prefix that at least `want` keys reach, bit by bit;
+// stops early once at most kEnough do.  Every thread returns it.
+__device__ unsigned long long key_prefix(const unsigned long long* keys, int n, int want, TopShared& sh, int& turn) {
     unsigned long long P = 0;
-    for (int bit = 63; bit >= last; --bit) {
+    for (int bit = 63; bit >= 0; --bit) {
         const unsigned long long cand = P | 1ull << bit;
         int c = 0;
-        for (int i = threadIdx.x; i < n; i += kLT) c += keys[i] >= cand;
-        c = block_sum(c, sh, turn);
+        for (int i = threadIdx.x; i < n; i += kNT) c += keys[i] >= cand;
+        c = block_sum(c, 0, sh, turn).x;
         if (c >= want) {
             P = cand;
-            if (c <= enough) break;
+            if (c <= kEnough) break;
         }
     }
     return P;
-}
-
-// The value a later candidate has to reach, given a prefix of 16 bits.
-__device__ __forceinline__ float prefix_value(unsigned long long P) {
-    const uint32_t o = (uint32_t)(P >> 32);
-    if (o <= 0x007fffffu) return -FLT_MAX;  // -inf is never a candidate
-    if (o > 0xff800000u) return kInf;
-    return value_of(o);
 }
 
 __device__ __forceinline__ void push(float x, int idx, TopShared& sh) {
@@ -279,44 +593,40 @@ __device__ __forceinline__ void push(float x, int idx, TopShared& sh) {
 // sh.best = the largest min(n, k) of sh.keys[0..n), in order; returns how many.
 __device__ int select_best(int n, int k, TopShared& sh, int& turn) {
     const int want = n < k ? n : k;
-    if (threadIdx.x == 0) sh.n_surv = 0;
-    if (want == 0) {
-        __syncthreads();
-        return 0;
+    const unsigned long long* from = sh.keys;
+    if (n > kEnough) {  // (the keys differ, so that at most kEnough reach the prefix in the end)
+        const unsigned long long P = key_prefix(sh.keys, n, want, sh, turn);
+        if (threadIdx.x == 0) sh.n_surv = 0;
+        consumers_sync();
+        for (int i = threadIdx.x; i < n; i += kNT)
+            if (sh.keys[i] >= P) sh.surv[atomicAdd(&sh.n_surv, 1)] = sh.keys[i];
+        consumers_sync();
+        n = sh.n_surv;
+        from = sh.surv;
     }
-    constexpr int room = 2 * kMaxList + 128;
-    const int enough = 2 * want + 64;  // <= room
-    const unsigned long long P = n > enough ? key_prefix(sh.keys, n, want, enough, 0, sh, turn) : 0ull;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kLT)
-        if (sh.keys[i] >= P) {
-            const int at = atomicAdd(&sh.n_surv, 1);
-            if (at < room) sh.surv[at] = sh.keys[i];
-        }
-    __syncthreads();
-    const int ns = sh.n_surv;  // the keys differ, so that at most `enough` reach the prefix
-    for (int i = threadIdx.x; i < ns; i += kLT) {
-        const unsigned long long me = sh.surv[i];
+    for (int i = threadIdx.x; i < n; i += kNT) {
+        const unsigned long long me = from[i];
         int above = 0;
-        for (int j = 0; j < ns; ++j) above += sh.surv[j] > me;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) above += from[j] > me;
         if (above < want) sh.best[above] = me;
     }
-    __syncthreads();
+    consumers_sync();
     return want;
 }
 
-// More candidates than the buffer holds (ascending rows, thousands of equal
-// values): the prefix is found digit by digit over the slice itself, eight bits
-// a pass, until at most kCand keys reach it; then they are collected again.
+// More candidates than the buffer holds (thousands of equal values): the prefix
+// is found digit by digit over the slice itself, eight bits a pass, until at most
+// kCand keys reach it; then they are collected again.
 template <int DT>
-__device__ int recollect(const Row<DT>& row, int v0, int v1, int k, TopShared& sh) {
+__device__ __noinline__ int recollect(const Row<DT>& row, int v0, int v1, int k, TopShared& sh) {
     constexpr int E = El<DT>::E;
     unsigned long long prefix = 0;
     int above = 0;  // keys known to lie above the prefix
     for (int shift = 56;; shift -= 8) {
-        sh.hist[threadIdx.x] = 0;
-        __syncthreads();
-        for (int vb = v0; vb < v1; vb += kLT) {
+        if (threadIdx.x < 256) sh.hist[threadIdx.x] = 0;
+        consumers_sync();
+        for (int vb = v0; vb < v1; vb += kNT) {
             const int v = vb + threadIdx.x;
             float x[E];
             El<DT>::unpack(row.load_if(v, v1), x);
@@ -333,7 +643,7 @@ __device__ int recollect(const Row<DT>& row, int v0, int v1, int k, TopShared& s
                 }
             }
         }
-        __syncthreads();
+        consumers_sync();
         if (threadIdx.x == 0) {
             int got = above, d = 255;
             while (d > 0 && got + (int)sh.hist[d] < k) got += (int)sh.hist[d--];
@@ -342,16 +652,16 @@ __device__ int recollect(const Row<DT>& row, int v0, int v1, int k, TopShared& s
             sh.n_surv = got;
             sh.n = 0;
         }
-        __syncthreads();
+        consumers_sync();
         prefix = sh.prefix;
         above = sh.n_surv;
         if (sh.done || shift == 0) {
             prefix <<= shift;
             break;
         }
-        __syncthreads();
+        consumers_sync();
     }
-    for (int v = v0 + threadIdx.x; v < v1; v += kLT) {
+    for (int v = v0 + threadIdx.x; v < v1; v += kNT) {
         float x[E];
         El<DT>::unpack(row.load(v), x);
 #pragma unroll 1
@@ -360,13 +670,110 @@ __device__ int recollect(const Row<DT>& row, int v0, int v1, int k, TopShared& s
             if (x[e] != -kInf && key_of(x[e], idx) >= prefix) push(x[e], idx, sh);
         }
     }
-    __syncthreads();
-    return sh.n;
+    consumers_sync();
+    const int n = sh.n;
+    consumers_sync();
+    return n;
+}
+
+// A bound that at least k of the groups' maxima reach (16-bit orders, two per
+// word of g; empty groups are 0), and few more: four candidates are counted per
+// barrier, first in growing steps below the slice's maximum, then between the
+// last that too few reached and the first that enough did.
+__device__ unsigned group_bound(const uint32_t (&g)[kMaxGroups / 2], unsigned top, int k, TopShared& ts, int& turn) {
+    const int few = k + k / 4 + 16;
+    int lo = 1, hi = (int)top + 1;  // enough reach lo (or there are not that many), too few reach hi
+    int at_lo = 1 << 30;
+    for (int step = 4; at_lo > few && hi - lo > 1;) {
+        int c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            c[i] = at_lo == 1 << 30 ? max(lo, (int)top - (step << (2 * i))) : lo + (int)((int64_t)(hi - lo) * (4 - i) / 5);
+        int n01 = 0, n23 = 0;
+#pragma unroll
+        for (int j = 0; j < kMaxGroups / 2; ++j) {
+            const int a = (int)(g[j] & 0xffffu), b = (int)(g[j] >> 16);
+            n01 += (a >= c[0]) + (b >= c[0]) + (((a >= c[1]) + (b >= c[1])) << 16);
+            n23 += (a >= c[2]) + (b >= c[2]) + (((a >= c[3]) + (b >= c[3])) << 16);
+        }
+        const int2 s = block_sum(n01, n23, ts, turn);
+        const int n[4] = {s.x & 0xffff, (int)((unsigned)s.x >> 16), s.y & 0xffff, (int)((unsigned)s.y >> 16)};
+        int found = 4;
+#pragma unroll
+        for (int i = 3; i >= 0; --i)
+            if (n[i] >= k) found = i;
+        if (found == 4) {
+            if (at_lo != 1 << 30 || c[3] > lo) hi = c[3];
+            else at_lo = 0;  // fewer than k groups at all: every one counts
+            step <<= 8;
+        } else {
+            if (found) hi = c[0];
+#pragma unroll
+            for (int i = 1; i < 4; ++i)
+                if (found > i) hi = c[i];
+            lo = c[0];
+            at_lo = n[0];
+#pragma unroll
+            for (int i = 1; i < 4; ++i)
+                if (found == i) lo = c[i], at_lo = n[i];
+        }
+    }
+    return (unsigned)lo;
+}
+
+// The best k tokens of a slice, given the maxima of its groups (ts.group) and its
+// largest value: a bound that at least k group maxima reach bounds the k-th best
+// element from below, and only the groups that reach it (k and a few) are read
+// again, from L2.  Group j of thread t: its vectors of chunks [j per, (j + 1) per).
+// Returns how many are in ts.best.
+template <int DT>
+__device__ int slice_best(const Slice<DT>& s, int groups, int per, float top, int k, TopShared& ts, int& turn) {
+    constexpr int E = El<DT>::E;
+    const int tid = threadIdx.x;
+    uint32_t g[kMaxGroups / 2];  // this thread's maxima, in pairs
+#pragma unroll
+    for (int j = 0; j < kMaxGroups / 2; ++j) {
+        g[j] = 0;
+        if (2 * j < groups) g[j] = ts.group[2 * j * kNT + tid];
+        if (2 * j + 1 < groups) g[j] |= (uint32_t)ts.group[(2 * j + 1) * kNT + tid] << 16;
+    }
+    const unsigned P = group_bound(g, order_of(top) >> 16, k, ts, turn);
+    // the lowest value of that order; nothing but -inf lies below the first
+    const float thr = P <= 0x7fu ? -FLT_MAX : value_of(P << 16);
+    const unsigned least = max(P, order_of(-FLT_MAX) >> 16);
+#pragma unroll
+    for (int j = 0; j < kMaxGroups; ++j)
+        if ((g[j / 2] >> (16 * (j & 1)) & 0xffffu) >= least) {
+            const int at = atomicAdd(&ts.n_hits, 1);
+            if (at < kMaxHits) ts.list[at] = j * kNT + tid;
+        }
+    consumers_sync();
+    const int hits = ts.n_hits;
+    int n = kCand + 1;
+    if (hits <= kMaxHits) {
+        const int vecs = per * kPer;  // of a group
+        for (int i = tid; i < hits * vecs; i += kNT) {
+            const int id = ts.list[i / vecs], q = i % vecs;
+            const int64_t v = s.v0 + ((int64_t)(id / kNT) * per * kPer + q) * kNT + id % kNT;
+            if (v >= s.v1) continue;
+            const uint4 w = s.row.load((int)v);
+            if (El<DT>::vmax(w) < thr) continue;
+            float x[E];
+            El<DT>::unpack(w, x);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (!(x[e] < thr)) push(x[e], (int)(v * E - s.row.mis + e), ts);
+        }
+        consumers_sync();
+        n = ts.n;
+    }
+    if (n > kCand) n = recollect<DT>(s.row, s.v0, s.v1, k, ts);
+    return select_best(n, k, ts, turn);
 }
 
 struct LogprobArgs {
     const void* logits;
-    int64_t ld;
+    int64_t ld, rows;
     int vocab, k;
     const int32_t* ids;
     float temperature;
@@ -374,151 +781,124 @@ struct LogprobArgs {
     int32_t* top_id;
 };
 
-// One row per cluster of `cs` CTAs.  Which elements can be among the k best is
-// decided with one comparison per vector: after the first batch the k-th
-// largest of the threads' maxima bounds the k-th best from below, and the bound
-// is raised from the collected candidates while they are many.  Per element the
-// pass spends about eight instructions; what bounds it is the read.
+// For the best tokens the pass keeps the maximum of every group of vectors, which
+// the running softmax needs anyway; slice_best does the rest.
 template <int DT, bool TOP>
-__global__ void __launch_bounds__(kLT) k_logprobs(LogprobArgs a, int cs) {
-    constexpr int E = El<DT>::E;
-    __shared__ RunShared rs;
-    __shared__ TopShared ts;
-    const int64_t r = blockIdx.x / cs;
-    const int rank = (int)(blockIdx.x % cs), tid = threadIdx.x;
-    const Row<DT> row(a.logits, a.ld, r, a.vocab);
-    const int v0 = (int)((int64_t)row.nv * rank / cs), v1 = (int)((int64_t)row.nv * (rank + 1) / cs);
-    const float c = 1.4426950408889634f / a.temperature;
-    Run run{-kInf, 0.f, 0.f};
-    float thr = -FLT_MAX;
-    int turn = 0;
-    if (TOP) {
-        if (tid < 3) ts.sum[tid] = 0;
-        if (tid == 3) ts.n = 0;
-        __syncthreads();
-    }
-    uint4 nxt[kLU];
-#pragma unroll
-    for (int u = 0; u < kLU; ++u) nxt[u] = row.load_if(v0 + tid + u * kLT, v1);
-    int it = 0;
-    for (int vb = v0; vb < v1; vb += kLT * kLU, ++it) {
-        uint4 cur[kLU];
-#pragma unroll
-        for (int u = 0; u < kLU; ++u) {
-            cur[u] = nxt[u];
-            nxt[u] = row.load_if(vb + tid + (kLU + u) * kLT, v1);
+__global__ void __launch_bounds__(kThreads, 2) k_logprobs(LogprobArgs a, int cs) {
+    extern __shared__ __align__(128) uint8_t l_smem[];
+    uint4* ring = reinterpret_cast<uint4*>(l_smem);
+    Link& l = *reinterpret_cast<Link*>(l_smem + kRingBytes);
+    TopShared& ts = *reinterpret_cast<TopShared*>(l_smem + kRingBytes + sizeof(Link));
+    const int rank = (int)(blockIdx.x % cs), tid = threadIdx.x, stride = gridDim.x / cs;
+    if (TOP && tid < 3) ts.sum[tid] = make_int2(0, 0);
+    link_init(l, cs);
+    Turn at;
+    if (tid >= kNT) {
+        if (tid == kNT) {
+            int64_t n = 0;
+            for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride)
+                if (!feed(Slice<DT>(a.logits, a.ld, r, a.vocab, rank, cs), ring, l, at, n)) break;
+            drain(l, at, n);
         }
-        float vm[kLU];
-#pragma unroll
-        for (int u = 0; u < kLU; ++u) vm[u] = El<DT>::vmax(cur[u]);
-        if (TOP) {
-            if (it == 0) {
-                float t = vm[0];
-#pragma unroll
-                for (int u = 1; u < kLU; ++u) t = max_nan(t, vm[u]);
-                ts.keys[tid] = (unsigned long long)order_of(t) << 32;
-                __syncthreads();
-                thr = a.k <= kLT ? prefix_value(key_prefix(ts.keys, kLT, a.k, a.k, 48, ts, turn)) : -FLT_MAX;
-                __syncthreads();
-            } else if ((it & (it - 1)) == 0) {
-                __syncthreads();
-                const int n = ts.n;
-                __syncthreads();  // nobody pushes before all have read it
-                if (n > 512 && n <= kCand) {
-                    thr = fmaxf(thr, prefix_value(key_prefix(ts.keys, n, a.k, a.k, 48, ts, turn)));
-                    __syncthreads();
-                }
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kLU; ++u) {
-            float x[E];
-            El<DT>::unpack(cur[u], x);
-            if (vm[u] > run.m) run_to(run, vm[u], c);
-            const float m = run.m == -kInf ? 0.f : run.m;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float t = (x[e] - m) * c, p = ex2(t);
-                run.s += p;
-                run.a = fmaf(p, fmaxf(t, -1e6f), run.a);  // (0 times -inf would be NaN)
-            }
-            if (TOP && !(vm[u] < thr)) {
-                const int base = (int)((int64_t)(vb + tid + u * kLT) * E - row.mis);
-#pragma unroll 1
-                for (int e = 0; e < E; ++e) {
-                    float y[E];
-                    El<DT>::unpack(cur[u], y);
-                    float xe = y[0];
-#pragma unroll
-                    for (int j = 1; j < E; ++j) xe = e == j ? y[j] : xe;
-                    if (!(xe < thr)) push(xe, base + e, ts);
-                }
-            }
-        }
-    }
-    run = run_reduce(run, rs, c, cs);
-    const float lns = logf(run.s), inv_t = 1.f / a.temperature;
-    const bool none = run.m == -kInf && run.s == 0.f;
-    if (rank == 0 && tid == 0) {
-        const float lse = none ? -kInf : fmaf(run.m, inv_t, lns);
-        if (a.lse) a.lse[r] = lse;
-        if (a.entropy) a.entropy[r] = none ? 0.f : lns - run.a / run.s * kLn2;
-        if (a.logprob) {
-            const int32_t id = a.ids[r];
-            float lp = 0.f;
-            if (id >= a.vocab) lp = __int_as_float(0x7fffffff);
-            else if (id >= 0) lp = none ? -kInf : (El<DT>::one(row.p[id]) - run.m) * inv_t - lns;
-            a.logprob[r] = lp;
-        }
-    }
-    if constexpr (!TOP) {
-        if (cs > 1) cg::this_cluster().sync();  // the others may still read this CTA's state
     } else {
-        __syncthreads();
-        int n = ts.n;
-        __syncthreads();
-        if (n > kCand) n = recollect<DT>(row, v0, v1, a.k, ts);
-        int nb = select_best(n, a.k, ts, turn);
-        if (cs > 1) {
-            cg::cluster_group cl = cg::this_cluster();
-            if (tid == 0) ts.n = nb;
-            cl.sync();
-            if (rank == 0) {
-                int at = 0;
-                for (int i = 0; i < cs; ++i) {
-                    const TopShared* o = cl.map_shared_rank(&ts, i);
-                    const int ni = o->n;
-                    for (int j = tid; j < ni; j += kLT) ts.keys[at + j] = o->best[j];
-                    at += ni;
+        const float inv_t = 1.f / a.temperature, c = 1.4426950408889634f / a.temperature;
+        int turn = 0, i = 0;
+        for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride, ++i) {
+            const Slice<DT> s(a.logits, a.ld, r, a.vocab, rank, cs);
+            const int chunks = s.chunks(), per = (chunks + kMaxGroups - 1) / kMaxGroups;
+            Acc<DT, true> acc;
+            int group = 0, in_group = 0;
+            float gm = -kInf;
+            bool ok = true;
+            if (TOP && tid == 0) ts.n = ts.n_hits = 0;
+            for (int b = 0; b < chunks; ++b) {
+                uint4 cur[kPer];
+                ok &= fetch(s, ring, l, at, s.v0 + b * kChunk, cur);
+#pragma unroll
+                for (int u = 0; u < kPer; ++u) {
+                    const float vm = El<DT>::vmax(cur[u]);
+                    acc.add(cur[u], vm, c);
+                    if (TOP) gm = max_nan(gm, vm);
                 }
-                n = at;
+                if (TOP && (++in_group == per || b + 1 == chunks)) {
+                    ts.group[group * kNT + tid] = (uint16_t)(order_of(gm) >> 16);
+                    ++group;
+                    in_group = 0;
+                    gm = -kInf;
+                }
             }
-            cl.sync();  // the others' lists have been read
-            if (rank != 0) return;
-            nb = select_best(n, a.k, ts, turn);
-        }
-        float* tl = a.top_logprob + r * a.k;
-        int32_t* ti = a.top_id + r * a.k;
-        for (int i = tid; i < nb; i += kLT) {
-            const unsigned long long key = ts.best[i];
-            const float x = value_of((uint32_t)(key >> 32));
-            ti[i] = (int32_t)(0xffffffffu - (uint32_t)key);
-            tl[i] = (x - run.m) * inv_t - lns;
-        }
-        if (nb < a.k && tid < 32) {  // fewer than k above -inf: the masked ones follow by index
-            int at = nb;
-            for (int b = 0; b < a.vocab && at < a.k; b += 32) {
-                const bool is = b + tid < a.vocab && El<DT>::one(row.p[b + tid]) == -kInf;
-                const unsigned vote = __ballot_sync(kFull, is);
-                const int mine = at + __popc(vote & ((1u << tid) - 1));
-                if (is && mine < a.k) {
-                    ti[mine] = b + tid;
-                    tl[mine] = none ? -kInf : (-kInf - run.m) * inv_t - lns;
+            Run mine = acc.get(), cta;
+            if (!ok) mine.s = kNan;
+            const Run run = row_reduce<DT>(mine, l, c, i, rank, cs, &cta);
+            const bool none = run.m == -kInf && run.s == 0.f;
+            const float lns = log_sum<DT>(run.s, run.m, c);
+            if (rank == 0 && tid == 0) {
+                if (a.lse) a.lse[r] = none ? -kInf : fmaf(run.m, inv_t, lns);
+                if (a.entropy) a.entropy[r] = none ? 0.f : logf(run.s) - run.a / run.s * kLn2;
+                if (a.logprob) {
+                    const int32_t id = a.ids[r];
+                    float lp = 0.f;
+                    if (id >= a.vocab) lp = kNan;
+                    else if (id >= 0) lp = none ? -kInf : (El<DT>::one(s.row.p[id]) - run.m) * inv_t - lns;
+                    a.logprob[r] = lp;
                 }
-                at += __popc(vote);
+            }
+            if constexpr (TOP) {
+                int nb = slice_best<DT>(s, group, per, cta.m, a.k, ts, turn);
+                if (cs > 1) {
+                    if (rank) {  // to the first CTA, which is past the row before once this row's sums are exchanged
+                        TopShared* o = cg::this_cluster().map_shared_rank(&ts, 0);
+                        for (int j = tid; j < nb; j += kNT) o->join[(rank - 1) * kMaxList + j] = ts.best[j];
+                        if (tid == 0) o->join_n[rank] = nb;
+                        asm volatile("fence.acq_rel.cluster;" ::: "memory");
+                        consumers_sync();
+                        if (tid == 0) arrive_at(&l.joined, 0);
+                        continue;
+                    }
+                    if (tid == 0) ts.done = wait(l, &l.joined, i & 1);
+                    consumers_sync();
+                    if (!ts.done) {
+                        for (int j = tid; j < a.k; j += kNT) {
+                            a.top_logprob[r * a.k + j] = kNan;
+                            a.top_id[r * a.k + j] = -1;
+                        }
+                        continue;
+                    }
+                    for (int j = tid; j < nb; j += kNT) ts.keys[j] = ts.best[j];
+                    int n = nb;
+                    for (int o = 1; o < cs; ++o) {
+                        const int no = ts.join_n[o];
+                        for (int j = tid; j < no; j += kNT) ts.keys[n + j] = ts.join[(o - 1) * kMaxList + j];
+                        n += no;
+                    }
+                    consumers_sync();
+                    nb = select_best(n, a.k, ts, turn);
+                }
+                float* tl = a.top_logprob + r * a.k;
+                int32_t* ti = a.top_id + r * a.k;
+                for (int j = tid; j < nb; j += kNT) {
+                    const unsigned long long key = ts.best[j];
+                    ti[j] = (int32_t)(0xffffffffu - (uint32_t)key);
+                    tl[j] = (value_of((uint32_t)(key >> 32)) - run.m) * inv_t - lns;
+                }
+                if (nb < a.k && tid < 32) {  // fewer than k above -inf: the masked ones follow by index
+                    int n = nb;
+                    for (int b = 0; b < a.vocab && n < a.k; b += 32) {
+                        const bool is = b + tid < a.vocab && El<DT>::one(s.row.p[b + tid]) == -kInf;
+                        const unsigned vote = __ballot_sync(kFull, is);
+                        const int to = n + __popc(vote & ((1u << tid) - 1));
+                        if (is && to < a.k) {
+                            ti[to] = b + tid;
+                            tl[to] = none ? -kInf : (-kInf - run.m) * inv_t - lns;
+                        }
+                        n += __popc(vote);
+                    }
+                }
             }
         }
     }
+    __syncwarp();
+    if (cs > 1) cg::this_cluster().sync();  // nobody's shared memory is written after it left
 }
 
 // ---------------------------------------------------------------- distillation
@@ -533,7 +913,7 @@ __global__ void __launch_bounds__(kLT) k_logprobs(LogprobArgs a, int cs) {
 // of the slice tells which are listed.
 struct DistillArgs {
     const void* logits;
-    int64_t ld;
+    int64_t ld, rows;
     int vocab, k, tail;
     const int32_t* ids;
     int64_t ld_ids;
@@ -547,36 +927,17 @@ struct DistillArgs {
     int64_t ld_grad;
 };
 
+// What a row's list gives by itself.
 struct ListShared {
-    int id[kMaxList];     // -1: absent
-    float x[kMaxList];    // the row's value there
-    float t[kMaxList];    // the teacher's value
-    double lq[kMaxList];  // log q
-    float q[kMaxList];
-    bool first[kMaxList]; // no earlier entry names this token
-    float4 coef;          // mo, alpha, M, Q / S
-    float loss;
+    double q[kMaxList], c;  // weights; sum of q (log q - x / T)
+    double sum, inv_t;      // sum of q
+    int id[kMaxList];       // -1: absent
+    float x[kMaxList];      // the row's value there
+    float t[kMaxList];      // the teacher's value
+    float merged[kMaxList]; // weight of the token, all its entries together
+    int next[kMaxList];     // -1 where an earlier entry names this token, else the entry itself
+    float q0, m, s;         // what the list leaves over; largest x, sum of powers relative to it
 };
-
-// The teacher's list of a row; an entry is absent if its token is outside the
-// vocabulary or its value is -inf.
-template <int DT>
-__device__ void list_load(const DistillArgs& a, const Row<DT>& row, int64_t r, ListShared& ls) {
-    for (int i = threadIdx.x; i < a.k; i += blockDim.x) {
-        const int id = a.ids[r * a.ld_ids + i];
-        const float t = a.teacher[r * a.ld_teacher + i];
-        const bool in = id >= 0 && id < a.vocab && t != -kInf;
-        ls.id[i] = in ? id : -1;
-        ls.t[i] = in ? t : -kInf;
-        ls.x[i] = in ? El<DT>::one(row.p[id]) : -kInf;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.k; i += blockDim.x) {
-        bool first = ls.id[i] >= 0;
-        for (int j = 0; j < i && first; ++j) first = ls.id[j] != ls.id[i];
-        ls.first[i] = first;
-    }
-}
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -588,216 +949,332 @@ __device__ __forceinline__ double warp_sum(double v) {
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
     return v;
 }
-__device__ __forceinline__ float warp_max(float v) {
+__device__ __forceinline__ float warp_max_nan(float v) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
+    for (int o = 16; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(kFull, v, o));
     return v;
 }
 
-// q and log q of the list (one warp); returns sum q.  In 64 bits, as the loss
-// below: it is a small difference of terms q log q and q log p, and q0 one of 1
-// and the sum.
-__device__ double list_weights(const DistillArgs& a, ListShared& ls) {
-    const int lane = threadIdx.x & 31;
-    double shift = 0.0;
-    if (!a.tail) {  // softmax over the list
-        float tm = -kInf;
-        for (int i = lane; i < a.k; i += 32) tm = fmaxf(tm, ls.t[i]);
-        tm = warp_max(tm);
-        if (tm == -kInf) tm = 0.f;
-        double z = 0.0;
-        for (int i = lane; i < a.k; i += 32) z += exp((double)ls.t[i] - tm);
-        z = warp_sum(z);
-        shift = tm + (z > 0.0 || z != z ? log(z) : 0.0);
-    }
-    double q = 0.0;
-    for (int i = lane; i < a.k; i += 32) {
-        ls.lq[i] = ls.t[i] - shift;
-        const double e = exp(ls.lq[i]);
-        ls.q[i] = (float)e;
-        q += e;
-    }
-    return warp_sum(q);
-}
-
-// Loss and gradient coefficients of a row from the unlisted elements' joined
-// softmax (one warp).
-__device__ void list_finish(const DistillArgs& a, const Run& o, float c, ListShared& ls) {
-    const int lane = threadIdx.x & 31;
-    int listed = 0;
-    for (int i = lane; i < a.k; i += 32) listed += ls.first[i];
-    listed = __reduce_add_sync(kFull, listed);
-    const double Q = list_weights(a, ls), inv_t = 1.0 / a.temperature;
-    double q0 = a.tail ? fmax(0.0, 1.0 - Q) : 0.0;
-    if (Q != Q) q0 = Q;  // a NaN in the list stays one
-    // nothing can be left over where the list covers the vocabulary; and where
-    // the rest is masked out, what rounding leaves of 1 - Q is nothing either
-    if (listed == a.vocab || (o.s == 0.f && q0 < a.k * 0x1p-22)) q0 = 0.0;
-    float M = o.m;
-    for (int i = lane; i < a.k; i += 32)
-        if (ls.id[i] >= 0) M = max_nan(M, ls.x[i]);
-#pragma unroll
-    for (int w = 16; w; w >>= 1) M = max_nan(M, __shfl_xor_sync(kFull, M, w));
-    const float ref = M == -kInf ? 0.f : M, mo = o.m == -kInf ? 0.f : o.m;
-    float in = 0.f;
-    for (int i = lane; i < a.k; i += 32)
-        if (ls.first[i]) in += ex2((ls.x[i] - ref) * c);
-    const float shrink = o.m == -kInf ? 0.f : ex2_full((o.m - ref) * c);  // unlisted powers relative to M
-    const float S = fmaf(o.s, shrink, warp_sum(in));
-    const bool none = S == 0.f;  // no finite logit in the row
-    const double lns = none ? 0.0 : log((double)S);
-    double loss = 0.0;
-    for (int i = lane; i < a.k; i += 32) {
-        const double q = exp(ls.lq[i]), lp = none ? -kInf : ((double)ls.x[i] - ref) * inv_t - lns;
-        if (q > 0.0 || q != q) loss += q * (ls.lq[i] - lp);
-    }
-    loss = warp_sum(loss);
-    if (lane == 0) {
-        if (q0 > 0.0 || q0 != q0)
-            loss += q0 * (log(q0) - (o.s == 0.f ? -kInf : ((double)o.m - ref) * inv_t + (log((double)o.s) - lns)));
-        ls.loss = (float)(loss * a.temperature * a.temperature);
-        const double Qt = Q + q0, k = none ? 0.0 : Qt / S;
-        ls.coef = make_float4(mo, o.s == 0.f ? 0.f : (float)(k * shrink - q0 / o.s), ref, (float)k);
-    }
-}
-
-// Writes the gradient of vectors [v0, v1) of the row, then the listed elements
-// among them.  f: the row's factor (weight times T).
+// Reads a row's list; thread `lane` of `threads`.  An entry is absent if its
+// token is outside the vocabulary or its value is -inf.
 template <int DT>
-__device__ void write_grad(const DistillArgs& a, const Row<DT>& row, int64_t r, int v0, int v1, float c, float f,
-                           const ListShared& ls) {
-    using T = typename El<DT>::T;
-    constexpr int E = El<DT>::E;
-    T* g = reinterpret_cast<T*>(a.grad) + r * a.ld_grad;
-    const bool aligned = (int)(((uintptr_t)g & 15) / sizeof(T)) == row.mis;
-    const float mo = ls.coef.x, alpha = ls.coef.y * f;
-    const bool zero = f == 0.f;  // rows outside the batch: zeros, whatever they hold
-    for (int vb = v0; vb < v1; vb += kLT * kLU) {
-        uint4 cur[kLU];
-#pragma unroll
-        for (int u = 0; u < kLU; ++u)
-            if (!zero) cur[u] = row.load_if(vb + threadIdx.x + u * kLT, v1);
-#pragma unroll
-        for (int u = 0; u < kLU; ++u) {
-            const int v = vb + threadIdx.x + u * kLT;
-            if (v >= v1) continue;
-            float x[E];
-            uint4 out = make_uint4(0, 0, 0, 0);
-            T* o = reinterpret_cast<T*>(&out);
-            if (!zero) {
-                El<DT>::unpack(cur[u], x);
-#pragma unroll
-                for (int e = 0; e < E; ++e) o[e] = El<DT>::put(alpha * ex2_full((x[e] - mo) * c));
-            }
-            const int64_t b = (int64_t)v * E - row.mis;
-            if (aligned && b >= 0 && b + E <= row.V) *reinterpret_cast<uint4*>(g + b) = out;
-            else
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (b + e >= 0 && b + e < row.V) g[b + e] = o[e];
-        }
-    }
-    if (zero) return;
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.k; i += kLT) {
-        const int id = ls.id[i], v = (id + row.mis) / E;
-        if (!ls.first[i] || v < v0 || v >= v1) continue;
-        float q = 0.f;
-        for (int j = i; j < a.k; ++j)
-            if (ls.id[j] == id) q += ls.q[j];
-        // (a row without a finite logit has no softmax: no gradient)
-        g[id] = El<DT>::put(ls.coef.w == 0.f ? 0.f : f * (ls.coef.w * ex2_full((ls.x[i] - ls.coef.z) * c) - q));
+__device__ __forceinline__ void list_read(const DistillArgs& a, const Row<DT>& row, int64_t r, ListShared& ls, int lane, int threads) {
+    for (int i = lane; i < a.k; i += threads) {
+        const int id = a.ids[r * a.ld_ids + i];
+        const float t = a.teacher[r * a.ld_teacher + i];
+        const bool in = id >= 0 && id < a.vocab && t != -kInf;
+        ls.id[i] = in ? id : -1;
+        ls.t[i] = in ? t : -kInf;
+        ls.x[i] = in ? El<DT>::one(row.p[id]) : -kInf;
     }
 }
 
-// Loss, statistics for a later backward pass and (GRAD) the gradient of one row
-// per cluster.  The gradient's second read of the row comes from L2.
-template <int DT, bool GRAD>
-__global__ void __launch_bounds__(kLT) k_distill(DistillArgs a, int cs) {
-    constexpr int E = El<DT>::E;
-    extern __shared__ uint32_t d_bits[];  // a bit per element of the slice: listed
-    __shared__ RunShared rs;
-    __shared__ ListShared ls;
-    const int64_t r = blockIdx.x / cs;
-    const int rank = (int)(blockIdx.x % cs), tid = threadIdx.x;
-    const Row<DT> row(a.logits, a.ld, r, a.vocab);
-    const int v0 = (int)((int64_t)row.nv * rank / cs), v1 = (int)((int64_t)row.nv * (rank + 1) / cs);
-    const float c = 1.4426950408889634f / a.temperature;
-    const int words = ((v1 - v0) * E + 31) / 32;
-    for (int i = tid; i < words; i += kLT) d_bits[i] = 0;
-    list_load<DT>(a, row, r, ls);
-    __syncthreads();
-    for (int i = tid; i < a.k; i += kLT) {
-        const int v = (ls.id[i] + row.mis) / E - v0;
-        if (ls.first[i] && v >= 0 && v < v1 - v0) {
-            const int b = v * E + (ls.id[i] + row.mis) % E;
-            atomicOr(&d_bits[b >> 5], 1u << (b & 31));
+// What follows from the list by itself (one warp).  The weights and the loss's
+// part are formed in 64 bits: the loss is a small difference of terms q log q and
+// q log p, and q0 one of 1 and sum q; this warp has the time of a row for it.
+template <int DT>
+__device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls) {
+    const int lane = threadIdx.x & 31;
+    float tm = -kInf, m = -kInf;
+    for (int i = lane; i < a.k; i += 32) {
+        tm = fmaxf(tm, ls.t[i]);
+        m = max_nan(m, ls.x[i]);
+    }
+    tm = warp_max_nan(tm);
+    m = warp_max_nan(m);
+    if (a.tail || tm == -kInf) tm = 0.f;
+    double z = 0.0;
+    float s = 0.f;
+    int listed = 0;
+    for (int i = lane; i < a.k; i += 32) {
+        const int id = ls.id[i];
+        bool first = id >= 0;
+        for (int j = 0; j < i && first; ++j) first = ls.id[j] != id;
+        ls.next[i] = first ? i : -1;
+        listed += first;
+        if (first) s += ex2(exponent<DT>(ls.x[i], m, c));
+        const double e = exp((double)ls.t[i] - tm);
+        ls.q[i] = e;
+        z += e;
+    }
+    z = warp_sum(z);
+    s = warp_sum(s);
+    listed = __reduce_add_sync(kFull, listed);
+    const double inv_t = 1.0 / (double)a.temperature;
+    const double scale = a.tail || z == 0.0 ? 1.0 : 1.0 / z, shift = a.tail || z == 0.0 ? 0.0 : tm + log(z);
+    double part = 0.0;
+    for (int i = lane; i < a.k; i += 32) {
+        const double q = ls.q[i] * scale;
+        ls.q[i] = q;
+        if (q > 0.0 || q != q) part += q * (((double)ls.t[i] - shift) - ls.x[i] * inv_t);
+    }
+    part = warp_sum(part);
+    __syncwarp();
+    for (int i = lane; i < a.k; i += 32) {
+        double q = 0.0;
+        if (ls.next[i] >= 0)
+            for (int j = i; j < a.k; ++j)
+                if (ls.id[j] == ls.id[i]) q += ls.q[j];
+        ls.merged[i] = (float)q;
+    }
+    if (lane == 0) {
+        ls.c = part;
+        ls.sum = z * scale;
+        ls.inv_t = inv_t;
+        ls.m = m;
+        ls.s = s;
+        double q0 = a.tail ? fmax(0.0, 1.0 - z) : 0.0;
+        if (listed == a.vocab) q0 = 0.0;  // nothing is left over
+        ls.q0 = z != z ? kNan : (float)q0;
+    }
+    __syncwarp();
+}
+
+// Gradient coefficients (x: mo, y: alpha, z: M, w: Q / S) of a row from its list
+// and the unlisted elements' softmax; *loss where it is asked for.
+template <int DT>
+__device__ __forceinline__ float4 row_finish(const DistillArgs& a, const Run& o, float c, const ListShared& ls, float* loss) {
+    // where the rest is masked out, what rounding leaves of 1 - sum q is nothing
+    const float q0 = o.s == 0.f && ls.q0 < (float)a.k * 0x1p-22f ? 0.f : ls.q0;
+    const float M = max_nan(o.m, ls.m);
+    const float up = o.m == -kInf ? 0.f : ex2_full(shift_of<DT>(o.m, M, c));  // the unlisted powers relative to M
+    const float ul = ls.m == -kInf ? 0.f : ex2_full(shift_of<DT>(ls.m, M, c));
+    const float S = fmaf(o.s, up, ls.s * ul), Q = (float)ls.sum;
+    const bool none = S == 0.f;  // no finite logit in the row
+    const float k = none ? 0.f : (Q + q0) / S;
+    if (loss) {
+        const double lse = none ? -kInf : M * ls.inv_t + (double)log_sum<DT>(S, M, c);
+        double v = none ? (Q > 0.f || q0 > 0.f ? (double)kInf : Q != Q ? (double)kNan : 0.0) : ls.c + ls.sum * lse;
+        if (!none && (q0 > 0.f || q0 != q0)) {
+            const double lse0 = o.s == 0.f ? -kInf : o.m * ls.inv_t + (double)log_sum<DT>(o.s, o.m, c);
+            v += q0 * ((double)logf(q0) - (lse0 - lse));
+        }
+        *loss = (float)(v * a.temperature * a.temperature);
+    }
+    return make_float4(o.m, o.s == 0.f ? 0.f : k * up - q0 / o.s, M, k);
+}
+
+// The gradient of an unlisted vector, alpha 2^((x - mo) c).
+template <int DT>
+struct GradOf {
+    float mo, c, alpha;
+    bool far;
+    f32x2 c2, r2, al2;
+    __device__ GradOf(float4 coef, float c, float f) : mo(coef.x), c(c), alpha(coef.y * f), far(wide<DT>(coef.x, c)) {
+        const float r = ref_of(mo, c);
+        c2 = pack2(c, c);
+        r2 = pack2(-r, -r);
+        al2 = pack2(alpha, alpha);
+    }
+    __device__ __forceinline__ uint4 operator()(const uint4& v) const {
+        constexpr int E = El<DT>::E;
+        float x[E];
+        El<DT>::unpack(v, x);
+        if (far) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = alpha * ex2_full((x[e] - mo) * c);
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                float t0, t1;
+                unpack2(fma2(pack2(x[e], x[e + 1]), c2, r2), t0, t1);
+                unpack2(mul2(pack2(El<DT>::power(t0), El<DT>::power(t1)), al2), x[e], x[e + 1]);
+            }
+        }
+        return El<DT>::pack(x);
+    }
+};
+
+// A row of the gradient: where vector v of the logits' row goes.
+template <int DT>
+struct GradRow {
+    using T = typename El<DT>::T;
+    T* g;
+    bool aligned;
+    __device__ GradRow(const DistillArgs& a, const Row<DT>& row, int64_t r) {
+        g = reinterpret_cast<T*>(a.grad) + r * a.ld_grad;
+        aligned = (int)(((uintptr_t)g & 15) / sizeof(T)) == row.mis;
+    }
+    __device__ __forceinline__ void put(const Row<DT>& row, int v, const uint4& out) const {
+        constexpr int E = El<DT>::E;
+        const int64_t b = (int64_t)v * E - row.mis;
+        if (aligned && b >= 0 && b + E <= row.V) {
+            __stcs(reinterpret_cast<uint4*>(g + b), out);
+            return;
+        }
+        const T* o = reinterpret_cast<const T*>(&out);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (b + e >= 0 && b + e < row.V) g[b + e] = o[e];
+    }
+    // The listed elements of vectors [v0, v1), over what put() left there.  (A row
+    // without a finite logit has no softmax: no gradient.)
+    __device__ void listed(const DistillArgs& a, const Row<DT>& row, int v0, int v1, float c, float f, float4 coef,
+                           const ListShared& ls, int threads) const {
+        for (int i = threadIdx.x; i < a.k; i += threads) {
+            const int id = ls.id[i], v = (id + row.mis) / El<DT>::E;
+            if (ls.next[i] < 0 || v < v0 || v >= v1) continue;
+            g[id] = El<DT>::put(coef.w == 0.f ? 0.f
+                                              : f * (coef.w * ex2_full(exponent<DT>(ls.x[i], coef.z, c)) - ls.merged[i]));
         }
     }
-    __syncthreads();
-    Run run{-kInf, 0.f, 0.f};
-    uint4 nxt[kLU];
+};
+
+// The vector with the elements of mask m out of the way.
+template <int DT>
+__device__ __noinline__ uint4 without(uint4 v, uint32_t m) {
+    float x[El<DT>::E];
+    El<DT>::unpack(v, x);
 #pragma unroll
-    for (int u = 0; u < kLU; ++u) nxt[u] = row.load_if(v0 + tid + u * kLT, v1);
-    for (int vb = v0; vb < v1; vb += kLT * kLU) {
-        uint4 cur[kLU];
-#pragma unroll
-        for (int u = 0; u < kLU; ++u) {
-            cur[u] = nxt[u];
-            nxt[u] = row.load_if(vb + tid + (kLU + u) * kLT, v1);
+    for (int e = 0; e < El<DT>::E; ++e)
+        if (m >> e & 1) x[e] = -kInf;
+    return El<DT>::pack(x);  // (what came from this type goes back unrounded)
+}
+
+// Loss, statistics for a later backward pass and (GRAD) the gradient.  The
+// gradient's second read of a row comes from L2: the rows in flight fit there
+// (cluster_size).
+template <int DT, bool GRAD>
+__global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) {
+    constexpr int E = El<DT>::E;
+    extern __shared__ __align__(128) uint8_t l_smem[];
+    uint4* ring = reinterpret_cast<uint4*>(l_smem);
+    Link& l = *reinterpret_cast<Link*>(l_smem + kRingBytes);
+    ListShared* lists = reinterpret_cast<ListShared*>(l_smem + kRingBytes + sizeof(Link));
+    uint32_t* bits = reinterpret_cast<uint32_t*>(lists + 2);  // a bit per element of the slice: listed
+    const int rank = (int)(blockIdx.x % cs), tid = threadIdx.x, stride = gridDim.x / cs;
+    const float c = 1.4426950408889634f / a.temperature;
+    for (int i = tid; i < slice_words(a.vocab, E, cs); i += kThreads) bits[i] = 0;
+    link_init(l, cs);
+    if (tid >= kNT) {
+        if (tid == kNT) {
+            Turn at;
+            int64_t n = 0;
+            for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride) {
+                const Slice<DT> s(a.logits, a.ld, r, a.vocab, rank, cs);
+                if (!feed(s, ring, l, at, n)) break;
+                if (GRAD && !(a.weight && a.weight[r] == 0.f) && !feed(s, ring, l, at, n)) break;
+            }
+            drain(l, at, n);
+        } else if (tid >= kNT + 32) {
+            int i = 0;
+            for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride, ++i) {
+                bool ok = i < 2 || wait(l, &l.list_empty[i & 1], ((i >> 1) - 1) & 1);
+                if (!__all_sync(kFull, ok)) break;
+                list_read<DT>(a, Row<DT>(a.logits, a.ld, r, a.vocab), r, lists[i & 1], tid & 31, 32);
+                __syncwarp();
+                list_prepare<DT>(a, c, lists[i & 1]);
+                if (tid == kNT + 32) u_mb_arrive(&l.list_full[i & 1]);
+            }
         }
-#pragma unroll
-        for (int u = 0; u < kLU; ++u) {
-            const int v = vb + tid + u * kLT - v0;
-            uint32_t m = 0;
-            if (v < v1 - v0) m = d_bits[(v * E) >> 5] >> ((v * E) & 31) & ((1u << E) - 1);
-            float x[E];
-            El<DT>::unpack(cur[u], x);
-            float vm = El<DT>::vmax(cur[u]);
-            if (m) {
-                vm = -kInf;
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    if (m >> e & 1) x[e] = -kInf;
-                    vm = max_nan(vm, x[e]);
+    } else {
+        Turn at;
+        int i = 0;
+        for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride, ++i) {
+            const Slice<DT> s(a.logits, a.ld, r, a.vocab, rank, cs);
+            const ListShared& ls = lists[i & 1];
+            bool ok = wait(l, &l.list_full[i & 1], (i >> 1) & 1);
+            int bit = -1;
+            if (ok && tid < a.k && ls.next[tid] >= 0) {
+                const int v = (ls.id[tid] + s.row.mis) / E - s.v0;
+                if (v >= 0 && v < s.v1 - s.v0) {
+                    bit = v * E + (ls.id[tid] + s.row.mis) % E;
+                    atomicOr(&bits[bit >> 5], 1u << (bit & 31));
                 }
             }
-            if (vm > run.m) run_to(run, vm, c);
-            const float ref = run.m == -kInf ? 0.f : run.m;
+            consumers_sync();
+            Acc<DT, false> acc;
+            for (int vb = s.v0; vb < s.v1; vb += kChunk) {
+                uint4 cur[kPer];
+                ok &= fetch(s, ring, l, at, vb, cur);
 #pragma unroll
-            for (int e = 0; e < E; ++e) run.s += ex2((x[e] - ref) * c);
+                for (int u = 0; u < kPer; ++u) {
+                    const int b = (vb + tid + u * kNT - s.v0) * E;
+                    const uint32_t m = b < (s.v1 - s.v0) * E ? bits[b >> 5] >> (b & 31) & ((1u << E) - 1) : 0;
+                    if (m) cur[u] = without<DT>(cur[u], m);
+                    acc.add(cur[u], El<DT>::vmax(cur[u]), c);
+                }
+            }
+            Run run = acc.get(), cta;
+            if (!ok) run.s = kNan;
+            run = row_reduce<DT>(run, l, c, i, rank, cs, &cta);
+            if (bit >= 0) bits[bit >> 5] = 0;  // (all are past the row; the next one's are set after the barrier below)
+            float loss;
+            const float4 coef = row_finish<DT>(a, run, c, ls, rank == 0 && tid == 0 ? &loss : nullptr);
+            if (rank == 0 && tid == 0) {
+                a.loss[r] = loss;
+                if (a.stats) a.stats[r] = coef;
+            }
+            if constexpr (GRAD) {
+                const float w = a.weight ? a.weight[r] : 1.f, f = w * a.temperature;
+                const GradRow<DT> out(a, s.row, r);
+                if (w == 0.f) {  // rows outside the batch: zeros, whatever they hold
+                    for (int v = s.v0 + tid; v < s.v1; v += kNT) out.put(s.row, v, make_uint4(0, 0, 0, 0));
+                } else {
+                    const GradOf<DT> grad(coef, c, f);
+                    for (int vb = s.v0; vb < s.v1; vb += kChunk) {
+                        uint4 cur[kPer];
+                        ok &= fetch(s, ring, l, at, vb, cur);
+#pragma unroll
+                        for (int u = 0; u < kPer; ++u) {
+                            const int v = vb + tid + u * kNT;
+                            uint4 o = grad(cur[u]);
+                            if (!ok) o = make_uint4(kFull, kFull, kFull, kFull);  // NaN in every type
+                            if (v < s.v1) out.put(s.row, v, o);
+                        }
+                    }
+                }
+                consumers_sync();
+                if (w != 0.f && ok) out.listed(a, s.row, s.v0, s.v1, c, f, coef, ls, kNT);
+            } else {
+                consumers_sync();
+            }
+            __syncwarp();
+            if ((tid & 31) == 0) u_mb_arrive(&l.list_empty[i & 1]);
         }
     }
-    run = run_reduce(run, rs, c, cs);
-    if (tid < 32) list_finish(a, run, c, ls);
-    __syncthreads();
-    if (rank == 0 && tid == 0) {
-        a.loss[r] = ls.loss;
-        if (a.stats) a.stats[r] = ls.coef;
-    }
-    if constexpr (GRAD) {
-        const float f = (a.weight ? a.weight[r] : 1.f) * a.temperature;
-        write_grad<DT>(a, row, r, v0, v1, c, f, ls);
-    }
-    if (cs > 1) cg::this_cluster().sync();  // the others may still read this CTA's state
+    __syncwarp();
+    if (cs > 1) cg::this_cluster().sync();  // nobody's shared memory is written after it left
 }
 
 // The gradient alone, from the forward pass's statistics: a CTA per chunk of a
-// row.
+// row, four vectors per thread in flight.
 template <int DT>
-__global__ void __launch_bounds__(kLT) k_distill_backward(DistillArgs a, int chunks) {
+__global__ void __launch_bounds__(kBT) k_distill_backward(DistillArgs a, int chunks) {
     __shared__ ListShared ls;
     const int64_t r = blockIdx.x / chunks;
     const int ch = (int)(blockIdx.x % chunks);
     const Row<DT> row(a.logits, a.ld, r, a.vocab);
     const int v0 = (int)((int64_t)row.nv * ch / chunks), v1 = (int)((int64_t)row.nv * (ch + 1) / chunks);
-    const float c = 1.4426950408889634f / a.temperature;
-    list_load<DT>(a, row, r, ls);
-    if (threadIdx.x == 0) ls.coef = a.stats[r];
+    const float c = 1.4426950408889634f / a.temperature, w = a.weight[r], f = w * a.temperature;
+    const GradRow<DT> out(a, row, r);
+    if (w == 0.f) {
+        for (int v = v0 + threadIdx.x; v < v1; v += kBT) out.put(row, v, make_uint4(0, 0, 0, 0));
+        return;
+    }
+    const float4 coef = a.stats[r];
+    const GradOf<DT> grad(coef, c, f);
+    uint4 nxt[kLU];
+#pragma unroll
+    for (int u = 0; u < kLU; ++u) nxt[u] = row.load_if(v0 + threadIdx.x + u * kBT, v1);
+    list_read<DT>(a, row, r, ls, threadIdx.x, kBT);
+    __syncthreads();  // the listed values are read before the row may be overwritten
+    if (threadIdx.x >= kBT - 32) list_prepare<DT>(a, c, ls);
+    for (int vb = v0; vb < v1; vb += kBT * kLU) {
+        uint4 cur[kLU];
+#pragma unroll
+        for (int u = 0; u < kLU; ++u) {
+            cur[u] = nxt[u];
+            nxt[u] = row.load_if(vb + threadIdx.x + (kLU + u) * kBT, v1);
+        }
+#pragma unroll
+        for (int u = 0; u < kLU; ++u) {
+            const int v = vb + threadIdx.x + u * kBT;
+            if (v < v1) out.put(row, v, grad(cur[u]));
+        }
+    }
     __syncthreads();
-    if (threadIdx.x < 32) list_weights(a, ls);
-    __syncthreads();
-    write_grad<DT>(a, row, r, v0, v1, c, a.weight[r] * a.temperature, ls);
+    out.listed(a, row, v0, v1, c, f, coef, ls, kBT);
 }
 
 // ---------------------------------------------------------------- host side
@@ -818,27 +1295,37 @@ int check_logits(const void* p, int type, int64_t rows, int vocab, int64_t ld, f
     if (type != EE_BF16 && type != EE_FP16 && type != EE_FP32) return fail(EE_EINVAL, "unknown element type");
     if (rows < 0 || vocab < 1 || vocab > EE_MAX_VOCAB) return fail(EE_EINVAL, "bad number of rows or vocabulary");
     if (ld < vocab) return fail(EE_EINVAL, "rows overlap: the row stride is below the vocabulary");
-    if (!(temperature >= 1e-6f && temperature <= 1e6f)) return fail(EE_EINVAL, "temperature must lie in 1e-6 to 1e6");
+    if (!(temperature >= EE_MIN_TEMPERATURE && temperature <= EE_MAX_TEMPERATURE))
+        return fail(EE_EINVAL, "temperature must lie in EE_MIN_TEMPERATURE to EE_MAX_TEMPERATURE");
     if (rows > 0x7fffffff / kMaxCluster) return fail(EE_EINVAL, "too many rows");
     if (rows && !p) return fail(EE_EINVAL, "NULL argument");
     if ((uintptr_t)p % elem_bytes(type)) return fail(EE_EINVAL, "logits are not aligned to their type");
     return EE_OK;
 }
 
-// CTAs per row: with fewer rows than two waves of one CTA per SM a row is shared
-// by a cluster, as long as every CTA keeps a batch of vectors.
-int cluster_size(int64_t rows, int vocab, int type, int n_sm) {
-    const int64_t vecs = (int64_t)vocab * (int64_t)elem_bytes(type) / 16;
+// CTAs per row: with fewer rows than CTAs that fit (two per SM) a row is shared
+// by a cluster, as long as every CTA keeps a stage of vectors.  A pass that reads
+// its rows twice shares them until the rows in flight fit in L2 beside what it
+// writes.
+int cluster_size(int64_t rows, int vocab, int type, int n_sm, bool twice) {
+    const int64_t bytes = (int64_t)vocab * (int64_t)elem_bytes(type), vecs = bytes / 16;
     int cs = 1;
-    while (cs < kMaxCluster && rows * cs < 2 * n_sm && vecs / (2 * cs) >= kLT * kLU) cs *= 2;
+    while (cs < kMaxCluster &&
+           ((vecs / (2 * cs) >= kChunk &&
+             (rows * cs < n_sm || (twice && bytes * std::min<int64_t>(rows, 2 * n_sm / cs) > kL2Rows))) ||
+            vocab / cs > kMaxSlice))
+        cs *= 2;
     return cs;
 }
 
 template <class K, class A>
-int launch_rows(K kern, int64_t rows, int cs, size_t smem, cudaStream_t s, const A& args) {
+int launch_rows(K kern, int64_t rows, int cs, int n_sm, size_t smem, cudaStream_t s, const A& args) {
+    // (one limit for every size: calls of other threads may set it too)
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    if (e != cudaSuccess) return cuda_status(e);
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(rows * cs));
-    cfg.blockDim = dim3(kLT);
+    cfg.gridDim = dim3((unsigned)(std::min<int64_t>(rows, std::max(1, 2 * n_sm / cs)) * cs));
+    cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
@@ -847,23 +1334,21 @@ int launch_rows(K kern, int64_t rows, int cs, size_t smem, cudaStream_t s, const
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = cs > 1 ? 1 : 0;
-    if (smem > 40 * 1024) {  // (one limit for every size: calls of other threads may set it too)
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxBits);
-        if (e != cudaSuccess) return cuda_status(e);
-    }
     return cuda_status(cudaLaunchKernelEx(&cfg, kern, args, cs));
 }
 
 template <int DT>
-int run_logprobs(const LogprobArgs& a, int64_t rows, int cs, cudaStream_t s) {
-    return a.k ? launch_rows(k_logprobs<DT, true>, rows, cs, 0, s, a)
-               : launch_rows(k_logprobs<DT, false>, rows, cs, 0, s, a);
+int run_logprobs(const LogprobArgs& a, int cs, int n_sm, cudaStream_t s) {
+    const size_t smem = kRingBytes + sizeof(Link);
+    return a.k ? launch_rows(k_logprobs<DT, true>, a.rows, cs, n_sm, smem + sizeof(TopShared), s, a)
+               : launch_rows(k_logprobs<DT, false>, a.rows, cs, n_sm, smem, s, a);
 }
 
 template <int DT>
-int run_distill(const DistillArgs& a, int64_t rows, int cs, size_t smem, cudaStream_t s) {
-    return a.grad ? launch_rows(k_distill<DT, true>, rows, cs, smem, s, a)
-                  : launch_rows(k_distill<DT, false>, rows, cs, smem, s, a);
+int run_distill(const DistillArgs& a, int cs, int n_sm, cudaStream_t s) {
+    const size_t smem = kRingBytes + sizeof(Link) + 2 * sizeof(ListShared) + 4 * (size_t)slice_words(a.vocab, El<DT>::E, cs);
+    return a.grad ? launch_rows(k_distill<DT, true>, a.rows, cs, n_sm, smem, s, a)
+                  : launch_rows(k_distill<DT, false>, a.rows, cs, n_sm, smem, s, a);
 }
 
 int check_list(const int32_t* ids, int64_t ld_ids, const float* teacher, int64_t ld_teacher, int k, int64_t rows) {
@@ -896,12 +1381,12 @@ int ee_token_logprobs(const void* logits, int type, int64_t rows, int vocab, int
     if ((logprob && !ids) || (k && (!top_logprob || !top_id))) return fail(EE_EINVAL, "NULL argument");
     int n_sm = 0;
     if ((rc = sm_count(&n_sm)) != EE_OK) return rc;
-    const LogprobArgs a{logits, ld, vocab, k, ids, temperature, logprob, entropy, lse, top_logprob, top_id};
-    const int cs = cluster_size(rows, vocab, type, n_sm);
+    const LogprobArgs a{logits, ld, rows, vocab, k, ids, temperature, logprob, entropy, lse, top_logprob, top_id};
+    const int cs = cluster_size(rows, vocab, type, n_sm, false);
     cudaStream_t s = (cudaStream_t)stream;
-    if (type == EE_BF16) return run_logprobs<EE_BF16>(a, rows, cs, s);
-    if (type == EE_FP16) return run_logprobs<EE_FP16>(a, rows, cs, s);
-    return run_logprobs<EE_FP32>(a, rows, cs, s);
+    if (type == EE_BF16) return run_logprobs<EE_BF16>(a, cs, n_sm, s);
+    if (type == EE_FP16) return run_logprobs<EE_FP16>(a, cs, n_sm, s);
+    return run_logprobs<EE_FP32>(a, cs, n_sm, s);
 }
 
 int ee_distill_topk(const void* logits, int type, int64_t rows, int vocab, int64_t ld, const int32_t* ids,
@@ -916,17 +1401,13 @@ int ee_distill_topk(const void* logits, int type, int64_t rows, int vocab, int64
     if ((uintptr_t)stats % 16) return fail(EE_EINVAL, "stats must be 16-byte aligned");
     int n_sm = 0;
     if ((rc = sm_count(&n_sm)) != EE_OK) return rc;
-    int cs = cluster_size(rows, vocab, type, n_sm);
-    // a bit per element of a slice, 128 KB at most
-    while (vocab / cs > EE_MAX_VOCAB / kMaxCluster) cs *= 2;
-    const int E = type == EE_FP32 ? 4 : 8;
-    const size_t smem = ((size_t)(vocab / E + 2) / cs + 1) * E / 8 + 8;
-    const DistillArgs a{logits, ld, vocab, k, tail ? 1 : 0, ids, ld_ids, teacher, ld_teacher, temperature, weight, loss,
+    const int cs = cluster_size(rows, vocab, type, n_sm, grad != nullptr);
+    const DistillArgs a{logits, ld, rows, vocab, k, tail ? 1 : 0, ids, ld_ids, teacher, ld_teacher, temperature, weight, loss,
                         reinterpret_cast<float4*>(stats), grad, ld_grad};
     cudaStream_t s = (cudaStream_t)stream;
-    if (type == EE_BF16) return run_distill<EE_BF16>(a, rows, cs, smem, s);
-    if (type == EE_FP16) return run_distill<EE_FP16>(a, rows, cs, smem, s);
-    return run_distill<EE_FP32>(a, rows, cs, smem, s);
+    if (type == EE_BF16) return run_distill<EE_BF16>(a, cs, n_sm, s);
+    if (type == EE_FP16) return run_distill<EE_FP16>(a, cs, n_sm, s);
+    return run_distill<EE_FP32>(a, cs, n_sm, s);
 }
 
 int ee_distill_topk_backward(const float* dloss, const void* logits, int type, int64_t rows, int vocab, int64_t ld,
@@ -940,17 +1421,17 @@ int ee_distill_topk_backward(const float* dloss, const void* logits, int type, i
     if (!rows) return EE_OK;
     if (!dloss || !stats || !grad) return fail(EE_EINVAL, "NULL argument");
     if ((uintptr_t)stats % 16) return fail(EE_EINVAL, "stats must be 16-byte aligned");
-    const DistillArgs a{logits, ld, vocab, k, tail ? 1 : 0, ids, ld_ids, teacher, ld_teacher, temperature, dloss, nullptr,
+    const DistillArgs a{logits, ld, rows, vocab, k, tail ? 1 : 0, ids, ld_ids, teacher, ld_teacher, temperature, dloss, nullptr,
                         reinterpret_cast<float4*>(const_cast<float*>(stats)), grad, ld_grad};
     // four batches of vectors per CTA
     const int64_t vecs = (int64_t)vocab * (int64_t)elem_bytes(type) / 16;
-    const int64_t chunks = std::max<int64_t>(1, vecs / (4 * kLT * kLU));
+    const int64_t chunks = std::max<int64_t>(1, vecs / (4 * kBT * kLU));
     if (rows * chunks > 0x7fffffff) return fail(EE_EINVAL, "too many rows");
     const unsigned grid = (unsigned)(rows * chunks);
     cudaStream_t s = (cudaStream_t)stream;
-    if (type == EE_BF16) k_distill_backward<EE_BF16><<<grid, kLT, 0, s>>>(a, (int)chunks);
-    else if (type == EE_FP16) k_distill_backward<EE_FP16><<<grid, kLT, 0, s>>>(a, (int)chunks);
-    else k_distill_backward<EE_FP32><<<grid, kLT, 0, s>>>(a, (int)chunks);
+    if (type == EE_BF16) k_distill_backward<EE_BF16><<<grid, kBT, 0, s>>>(a, (int)chunks);
+    else if (type == EE_FP16) k_distill_backward<EE_FP16><<<grid, kBT, 0, s>>>(a, (int)chunks);
+    else k_distill_backward<EE_FP32><<<grid, kBT, 0, s>>>(a, (int)chunks);
     return cuda_status(cudaGetLastError());
 }
 
