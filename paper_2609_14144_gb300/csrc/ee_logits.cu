@@ -39,9 +39,6 @@ constexpr float kInf = __builtin_huge_valf();
 constexpr float kNan = __builtin_nanf("");
 constexpr unsigned kFull = 0xffffffffu;
 
-// Words of a slice's listed bits.
-__host__ __device__ inline int slice_words(int vocab, int E, int cs) { return (((vocab / E + 2) / cs + 1) * E + 31) / 32 + 1; }
-
 __device__ __forceinline__ float ex2(float t) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
@@ -79,6 +76,13 @@ struct El<EE_BF16> {
         const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
         const __nv_bfloat162 a = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
         return max_nan(__low2float(a), __high2float(a));
+    }
+    static __device__ __forceinline__ uint4 max4(uint4 a, const uint4& b) {
+        __nv_bfloat162* x = reinterpret_cast<__nv_bfloat162*>(&a);
+        const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __hmax2_nan(x[i], y[i]);
+        return a;
     }
     // Elements no lower than a value whose power is 0 beside any maximum that is not wide.
     static __device__ __forceinline__ uint4 floor(uint4 v) {
@@ -119,6 +123,13 @@ struct El<EE_FP16> {
         const __half2 a = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
         return max_nan(__low2float(a), __high2float(a));
     }
+    static __device__ __forceinline__ uint4 max4(uint4 a, const uint4& b) {
+        __half2* x = reinterpret_cast<__half2*>(&a);
+        const __half2* y = reinterpret_cast<const __half2*>(&b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __hmax2_nan(x[i], y[i]);
+        return a;
+    }
     static __device__ __forceinline__ uint4 floor(uint4 v) {
         __half2* h = reinterpret_cast<__half2*>(&v);
         const __half2 lo = __float2half2_rn(-65504.f);
@@ -152,6 +163,13 @@ struct El<EE_FP32> {
         return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)),
                        max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
     }
+    static __device__ __forceinline__ uint4 max4(uint4 a, const uint4& b) {
+        uint32_t* x = reinterpret_cast<uint32_t*>(&a);
+        const uint32_t* y = reinterpret_cast<const uint32_t*>(&b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __float_as_uint(max_nan(__uint_as_float(x[i]), __uint_as_float(y[i])));
+        return a;
+    }
     static __device__ __forceinline__ uint4 floor(uint4 v) {
         uint32_t* w = reinterpret_cast<uint32_t*>(&v);
 #pragma unroll
@@ -165,6 +183,15 @@ struct El<EE_FP32> {
     }
     static __device__ __forceinline__ float power(float t) { return ex2_full(t); }
 };
+
+// The largest element of several vectors, NaN if there is one.
+template <int DT, int N>
+__device__ __forceinline__ float max_of(const uint4 (&v)[N]) {
+    uint4 m = v[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) m = El<DT>::max4(m, v[i]);
+    return El<DT>::vmax(m);
+}
 
 // A row as 16-byte vectors: vector v holds elements [v E - mis, v E - mis + E)
 // of the row, mis being how many elements lie between a 16-byte boundary and
@@ -277,45 +304,62 @@ struct Acc {
         run_to<DT>(q, vm, c);
         return q;
     }
-    // Adds a vector whose largest element is vm (NaN if it holds one).
-    __device__ __forceinline__ void add(uint4 v, float vm, float c) {
+    // Adds vectors whose largest element is vm (NaN if there is one).
+    template <int N>
+    __device__ __forceinline__ void add(uint4 (&v)[N], float vm, float c) {
         constexpr int E = El<DT>::E;
-        if (vm > m) {
-            const Run q = moved(get(), vm, c);
-            m = q.m;
-            s = pack2(q.s, 0.f);
-            a = pack2(q.a, 0.f);
-            r = ref_of(m, c);
-            far = wide<DT>(m, c);
-        }
-        float x[E];
-        if (far) {
-            El<DT>::unpack(v, x);
-            float p = 0.f, q = 0.f;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float t = (x[e] - m) * c, w = ex2(t);
-                p += w;
-                q = fmaf(w, fmaxf(t, -1e6f), q);
+        if (!(vm <= m) || far) {
+            if (vm > m) {
+                const Run q = moved(get(), vm, c);
+                m = q.m;
+                s = pack2(q.s, 0.f);
+                a = pack2(q.a, 0.f);
+                r = ref_of(m, c);
+                far = wide<DT>(m, c);
             }
-            s = add2(s, pack2(p, 0.f));
-            if (ENT) a = add2(a, pack2(q, 0.f));
-            return;
+            if (far) {
+#pragma unroll 1
+                for (int u = 0; u < N; ++u) {
+                    uint4 w = v[0];
+#pragma unroll
+                    for (int j = 1; j < N; ++j) w = u == j ? v[j] : w;
+                    const float2 f = far_sums(w, m, c);
+                    s = add2(s, pack2(f.x, 0.f));
+                    if (ENT) a = add2(a, pack2(f.y, 0.f));
+                }
+                return;
+            }
         }
-        if (ENT) v = El<DT>::floor(v);  // -inf times its power 0 would be NaN
-        El<DT>::unpack(v, x);
         const f32x2 c2 = pack2(c, c), r2 = pack2(-r, -r);
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-            const f32x2 t = fma2(pack2(x[e], x[e + 1]), c2, r2);
-            float t0, t1;
-            unpack2(t, t0, t1);
-            const f32x2 p = pack2(ex2(t0), ex2(t1));
-            s = add2(s, p);
-            if (ENT) a = fma2(p, t, a);
+        for (int u = 0; u < N; ++u) {
+            float x[E];
+            El<DT>::unpack(ENT ? El<DT>::floor(v[u]) : v[u], x);  // (-inf times its power 0 would be NaN)
+#pragma unroll
+            for (int e = 0; e < E; e += 2) {
+                const f32x2 t = fma2(pack2(x[e], x[e + 1]), c2, r2);
+                float t0, t1;
+                unpack2(t, t0, t1);
+                const f32x2 p = pack2(ex2(t0), ex2(t1));
+                s = add2(s, p);
+                if (ENT) a = fma2(p, t, a);
+            }
         }
     }
+    __device__ __noinline__ static float2 far_sums(uint4 v, float m, float c) {
+        constexpr int E = El<DT>::E;
+        float x[E], p = 0.f, q = 0.f;
+        El<DT>::unpack(v, x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float t = (x[e] - m) * c, w = ex2(t);
+            p += w;
+            q = fmaf(w, fmaxf(t, -1e6f), q);
+        }
+        return make_float2(p, q);
+    }
 };
+
 // ---------------------------------------------------------------- streaming
 // A cluster of `cs` CTAs takes rows one after the other, each CTA a slice of the
 // row's vectors.  One warp of a CTA keeps a ring of shared-memory stages filled
@@ -323,15 +367,25 @@ struct Acc {
 // stays busy while the others reduce, select or write; twelve warps consume; one
 // more prepares the next row's list where there is one.  Two CTAs fit an SM.
 // Loading through registers instead (four vectors per thread, one batch ahead)
-// reached 4.7 TB/s in the stream and nothing between: 219 us where a pass over
-// 2048 x 151936 bf16 takes 92 us of reading.
+// reached 4.7 TB/s in the stream and nothing between rows: 219 us where a pass
+// over 2048 x 151936 bf16 takes 92 us of reading.  What is left to watch is the
+// number of instructions per element (a budget of about 11 per element of two
+// bytes): a chunk that lies wholly in the slice has one wait, one comparison and
+// no other condition.
 constexpr int kNT = 384;                 // consuming threads
 constexpr int kWarps = kNT / 32;
 constexpr int kThreads = kNT + 64;
-constexpr int kPer = 2;                  // vectors per thread and chunk
-constexpr int kChunk = kNT * kPer;       // vectors per stage: 12 KB
-constexpr int kStages = 6;
+constexpr int kPer = 4;                  // vectors per thread and chunk
+constexpr int kChunk = kNT * kPer;       // vectors per stage: 24 KB
+constexpr int kStages = 3;
 constexpr int kRingBytes = kStages * kChunk * 16;
+
+// Words of a slice's listed bits and of the flags over them.
+__host__ __device__ inline int slice_vecs(int vocab, int E, int cs) { return (vocab / E + 2) / cs + 1; }
+__host__ __device__ inline int slice_words(int vocab, int E, int cs) { return (slice_vecs(vocab, E, cs) * E + 31) / 32 + 1; }
+__host__ __device__ inline int slice_flags(int vocab, int E, int cs) {
+    return (slice_vecs(vocab, E, cs) + kChunk - 1) / kChunk * kWarps;
+}
 
 __device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 384;" ::: "memory"); }
 static_assert(kNT == 384, "consumers_sync");
@@ -420,6 +474,8 @@ struct Slice {
         f0 = row.mis ? 1 : 0;
         f1 = (int)(((int64_t)row.V + row.mis) / El<DT>::E);
     }
+    // The chunk at vb lies wholly in the slice and in the row.
+    __device__ __forceinline__ bool inner(int vb) const { return vb >= f0 && vb + kChunk <= min(f1, v1); }
     __device__ int chunks() const { return (v1 - v0 + kChunk - 1) / kChunk; }
 };
 
@@ -453,12 +509,17 @@ template <int DT>
 __device__ __forceinline__ bool fetch(const Slice<DT>& s, const uint4* ring, Link& l, Turn& t, int vb, uint4 (&cur)[kPer]) {
     const bool ok = wait(l, &l.full[t.st], t.ph);
     const uint4* st = ring + t.st * kChunk + threadIdx.x;
+    if (s.inner(vb)) {
 #pragma unroll
-    for (int u = 0; u < kPer; ++u) {
-        const int v = vb + threadIdx.x + u * kNT;
-        if (v >= s.f0 && v < s.f1 && v < s.v1) cur[u] = st[u * kNT];
-        else if (v < s.v1) cur[u] = s.row.load_edge((int64_t)v * El<DT>::E - s.row.mis);
-        else cur[u] = make_uint4(El<DT>::ninf, El<DT>::ninf, El<DT>::ninf, El<DT>::ninf);
+        for (int u = 0; u < kPer; ++u) cur[u] = st[u * kNT];
+    } else {
+#pragma unroll
+        for (int u = 0; u < kPer; ++u) {
+            const int v = vb + threadIdx.x + u * kNT;
+            if (v >= s.f0 && v < s.f1 && v < s.v1) cur[u] = st[u * kNT];
+            else if (v < s.v1) cur[u] = s.row.load_edge((int64_t)v * El<DT>::E - s.row.mis);
+            else cur[u] = make_uint4(El<DT>::ninf, El<DT>::ninf, El<DT>::ninf, El<DT>::ninf);
+        }
     }
     __syncwarp();
     if ((threadIdx.x & 31) == 0) u_mb_arrive(&l.empty[t.st]);
@@ -814,12 +875,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_logprobs(LogprobArgs a, int cs)
             for (int b = 0; b < chunks; ++b) {
                 uint4 cur[kPer];
                 ok &= fetch(s, ring, l, at, s.v0 + b * kChunk, cur);
-#pragma unroll
-                for (int u = 0; u < kPer; ++u) {
-                    const float vm = El<DT>::vmax(cur[u]);
-                    acc.add(cur[u], vm, c);
-                    if (TOP) gm = max_nan(gm, vm);
-                }
+                const float vm = max_of<DT>(cur);
+                acc.add(cur, vm, c);
+                if (TOP) gm = max_nan(gm, vm);
                 if (TOP && (++in_group == per || b + 1 == chunks)) {
                     ts.group[group * kNT + tid] = (uint16_t)(order_of(gm) >> 16);
                     ++group;
@@ -1070,17 +1128,20 @@ struct GradOf {
         constexpr int E = El<DT>::E;
         float x[E];
         El<DT>::unpack(v, x);
-        if (far) {
+        if (far) return of_far(v, mo, c, alpha);
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = alpha * ex2_full((x[e] - mo) * c);
-        } else {
-#pragma unroll
-            for (int e = 0; e < E; e += 2) {
-                float t0, t1;
-                unpack2(fma2(pack2(x[e], x[e + 1]), c2, r2), t0, t1);
-                unpack2(mul2(pack2(El<DT>::power(t0), El<DT>::power(t1)), al2), x[e], x[e + 1]);
-            }
+        for (int e = 0; e < E; e += 2) {
+            float t0, t1;
+            unpack2(fma2(pack2(x[e], x[e + 1]), c2, r2), t0, t1);
+            unpack2(mul2(pack2(El<DT>::power(t0), El<DT>::power(t1)), al2), x[e], x[e + 1]);
         }
+        return El<DT>::pack(x);
+    }
+    __device__ __noinline__ static uint4 of_far(uint4 v, float mo, float c, float alpha) {
+        float x[El<DT>::E];
+        El<DT>::unpack(v, x);
+#pragma unroll
+        for (int e = 0; e < El<DT>::E; ++e) x[e] = alpha * ex2_full((x[e] - mo) * c);
         return El<DT>::pack(x);
     }
 };
@@ -1141,10 +1202,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) 
     uint4* ring = reinterpret_cast<uint4*>(l_smem);
     Link& l = *reinterpret_cast<Link*>(l_smem + kRingBytes);
     ListShared* lists = reinterpret_cast<ListShared*>(l_smem + kRingBytes + sizeof(Link));
-    uint32_t* bits = reinterpret_cast<uint32_t*>(lists + 2);  // a bit per element of the slice: listed
+    // which vectors of a warp's in a chunk hold listed elements; a bit per element
+    uint32_t* flags = reinterpret_cast<uint32_t*>(lists + 2);
+    uint32_t* bits = flags + slice_flags(a.vocab, E, cs);
     const int rank = (int)(blockIdx.x % cs), tid = threadIdx.x, stride = gridDim.x / cs;
     const float c = 1.4426950408889634f / a.temperature;
-    for (int i = tid; i < slice_words(a.vocab, E, cs); i += kThreads) bits[i] = 0;
+    for (int i = tid; i < slice_flags(a.vocab, E, cs) + slice_words(a.vocab, E, cs); i += kThreads) flags[i] = 0;
     link_init(l, cs);
     if (tid >= kNT) {
         if (tid == kNT) {
@@ -1174,31 +1237,36 @@ __global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) 
             const Slice<DT> s(a.logits, a.ld, r, a.vocab, rank, cs);
             const ListShared& ls = lists[i & 1];
             bool ok = wait(l, &l.list_full[i & 1], (i >> 1) & 1);
-            int bit = -1;
+            int bit = -1, flag = 0;
             if (ok && tid < a.k && ls.next[tid] >= 0) {
                 const int v = (ls.id[tid] + s.row.mis) / E - s.v0;
                 if (v >= 0 && v < s.v1 - s.v0) {
                     bit = v * E + (ls.id[tid] + s.row.mis) % E;
+                    flag = v / kChunk * kWarps + v % kNT / 32;
                     atomicOr(&bits[bit >> 5], 1u << (bit & 31));
+                    atomicOr(&flags[flag], 1u << (v % kChunk / kNT));
                 }
             }
             consumers_sync();
             Acc<DT, false> acc;
-            for (int vb = s.v0; vb < s.v1; vb += kChunk) {
+            for (int vb = s.v0, b = 0; vb < s.v1; vb += kChunk, ++b) {
                 uint4 cur[kPer];
                 ok &= fetch(s, ring, l, at, vb, cur);
+                const uint32_t here = flags[b * kWarps + (tid >> 5)];  // (alike for the warp)
+                if (here) {
 #pragma unroll
-                for (int u = 0; u < kPer; ++u) {
-                    const int b = (vb + tid + u * kNT - s.v0) * E;
-                    const uint32_t m = b < (s.v1 - s.v0) * E ? bits[b >> 5] >> (b & 31) & ((1u << E) - 1) : 0;
-                    if (m) cur[u] = without<DT>(cur[u], m);
-                    acc.add(cur[u], El<DT>::vmax(cur[u]), c);
+                    for (int u = 0; u < kPer; ++u)
+                        if (here >> u & 1) {
+                            const int e = (vb - s.v0 + tid + u * kNT) * E;
+                            if (e < (s.v1 - s.v0) * E) cur[u] = without<DT>(cur[u], bits[e >> 5] >> (e & 31) & ((1u << E) - 1));
+                        }
                 }
+                acc.add(cur, max_of<DT>(cur), c);
             }
             Run run = acc.get(), cta;
             if (!ok) run.s = kNan;
             run = row_reduce<DT>(run, l, c, i, rank, cs, &cta);
-            if (bit >= 0) bits[bit >> 5] = 0;  // (all are past the row; the next one's are set after the barrier below)
+            if (bit >= 0) bits[bit >> 5] = flags[flag] = 0;  // (all are past the row; the next one's are set after the barrier below)
             float loss;
             const float4 coef = row_finish<DT>(a, run, c, ls, rank == 0 && tid == 0 ? &loss : nullptr);
             if (rank == 0 && tid == 0) {
@@ -1215,12 +1283,20 @@ __global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) 
                     for (int vb = s.v0; vb < s.v1; vb += kChunk) {
                         uint4 cur[kPer];
                         ok &= fetch(s, ring, l, at, vb, cur);
+                        if (s.inner(vb) && out.aligned && ok) {
+                            uint4* to = reinterpret_cast<uint4*>(out.g + ((int64_t)(vb + tid) * E - s.row.mis));
 #pragma unroll
-                        for (int u = 0; u < kPer; ++u) {
-                            const int v = vb + tid + u * kNT;
-                            uint4 o = grad(cur[u]);
-                            if (!ok) o = make_uint4(kFull, kFull, kFull, kFull);  // NaN in every type
-                            if (v < s.v1) out.put(s.row, v, o);
+                            for (int u = 0; u < kPer; ++u) __stcs(to + u * kNT, grad(cur[u]));
+                        } else {
+#pragma unroll 1
+                            for (int u = 0; u < kPer; ++u) {
+                                const int v = vb + tid + u * kNT;
+                                uint4 w4 = cur[0];
+#pragma unroll
+                                for (int j = 1; j < kPer; ++j) w4 = u == j ? cur[j] : w4;
+                                w4 = ok ? grad(w4) : make_uint4(kFull, kFull, kFull, kFull);  // NaN in every type
+                                if (v < s.v1) out.put(s.row, v, w4);
+                            }
                         }
                     }
                 }
@@ -1346,7 +1422,7 @@ int run_logprobs(const LogprobArgs& a, int cs, int n_sm, cudaStream_t s) {
 
 template <int DT>
 int run_distill(const DistillArgs& a, int cs, int n_sm, cudaStream_t s) {
-    const size_t smem = kRingBytes + sizeof(Link) + 2 * sizeof(ListShared) + 4 * (size_t)slice_words(a.vocab, El<DT>::E, cs);
+    const size_t smem = kRingBytes + sizeof(Link) + 2 * sizeof(ListShared) + 4 * (size_t)(slice_flags(a.vocab, El<DT>::E, cs) + slice_words(a.vocab, El<DT>::E, cs));
     return a.grad ? launch_rows(k_distill<DT, true>, a.rows, cs, n_sm, smem, s, a)
                   : launch_rows(k_distill<DT, false>, a.rows, cs, n_sm, smem, s, a);
 }
