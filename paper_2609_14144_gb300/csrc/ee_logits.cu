@@ -77,6 +77,16 @@ struct El<EE_BF16> {
         const __nv_bfloat162 a = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
         return max_nan(__low2float(a), __high2float(a));
     }
+    // The vector with the elements of mask m at -inf.
+    static __device__ __forceinline__ uint4 without(uint4 v, uint32_t m) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t k = (m >> (2 * i) & 1 ? 0xffffu : 0u) | (m >> (2 * i) & 2 ? 0xffff0000u : 0u);
+            w[i] = (w[i] & ~k) | (ninf & k);
+        }
+        return v;
+    }
     static __device__ __forceinline__ uint4 max4(uint4 a, const uint4& b) {
         __nv_bfloat162* x = reinterpret_cast<__nv_bfloat162*>(&a);
         const __nv_bfloat162* y = reinterpret_cast<const __nv_bfloat162*>(&b);
@@ -123,6 +133,16 @@ struct El<EE_FP16> {
         const __half2 a = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
         return max_nan(__low2float(a), __high2float(a));
     }
+    // The vector with the elements of mask m at -inf.
+    static __device__ __forceinline__ uint4 without(uint4 v, uint32_t m) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t k = (m >> (2 * i) & 1 ? 0xffffu : 0u) | (m >> (2 * i) & 2 ? 0xffff0000u : 0u);
+            w[i] = (w[i] & ~k) | (ninf & k);
+        }
+        return v;
+    }
     static __device__ __forceinline__ uint4 max4(uint4 a, const uint4& b) {
         __half2* x = reinterpret_cast<__half2*>(&a);
         const __half2* y = reinterpret_cast<const __half2*>(&b);
@@ -162,6 +182,15 @@ struct El<EE_FP32> {
     static __device__ __forceinline__ float vmax(const uint4& v) {
         return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)),
                        max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+    }
+    // The vector with the elements of mask m at -inf.
+    static __device__ __forceinline__ uint4 without(uint4 v, uint32_t m) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (m >> i & 1) w[i] = ninf;
+        }
+        return v;
     }
     static __device__ __forceinline__ uint4 max4(uint4 a, const uint4& b) {
         uint32_t* x = reinterpret_cast<uint32_t*>(&a);
@@ -273,12 +302,12 @@ template <int DT>
 __device__ __forceinline__ float shift_of(float m1, float m2, float c) {
     return wide<DT>(m1, c) || wide<DT>(m2, c) ? (m1 - m2) * c : ref_of(m1, c) - ref_of(m2, c);
 }
-// m: largest value so far (-inf: none); s: sum of 2^t; a: sum of t 2^t, from
-// which the entropy follows.
+// m: the reference, a value near the largest so far (-inf: none); s: sum of 2^t;
+// a: sum of t 2^t, from which the entropy follows.
 struct Run {
     float m, s, a;
 };
-// Rescale to the larger maximum m2.
+// Rescale to the larger reference m2.
 template <int DT>
 __device__ __forceinline__ void run_to(Run& r, float m2, float c) {
     if (r.m != -kInf) {  // (before the first value s is 0, or NaN if one was seen)
@@ -291,7 +320,7 @@ __device__ __forceinline__ void run_to(Run& r, float m2, float c) {
 // A thread's running softmax: the sums in pairs.
 template <int DT, bool ENT>
 struct Acc {
-    float m = -kInf, r = 0.f;
+    float m = -kInf, r = 0.f, lim = -kInf;
     bool far = false;  // wide(m)
     f32x2 s = 0, a = 0;
     __device__ __forceinline__ Run get() const {
@@ -308,14 +337,18 @@ struct Acc {
     template <int N>
     __device__ __forceinline__ void add(uint4 (&v)[N], float vm, float c) {
         constexpr int E = El<DT>::E;
-        if (!(vm <= m) || far) {
-            if (vm > m) {
+        // A new reference only when the largest power would pass 2^20: the first chunk
+        // sets it, and most threads keep it (following every new maximum, some lane
+        // of a warp did in nearly every chunk).
+        if (!(vm <= lim) || far) {
+            if (vm > lim || (far && vm > m)) {
                 const Run q = moved(get(), vm, c);
                 m = q.m;
                 s = pack2(q.s, 0.f);
                 a = pack2(q.a, 0.f);
                 r = ref_of(m, c);
                 far = wide<DT>(m, c);
+                lim = m + 20.f / c;
             }
             if (far) {
 #pragma unroll 1
@@ -504,31 +537,45 @@ __device__ void drain(Link& l, Turn t, int64_t n) {
     }
 }
 
-// This thread's vectors of the chunk at vb, and the stage's release.
-template <int DT>
-__device__ __forceinline__ bool fetch(const Slice<DT>& s, const uint4* ring, Link& l, Turn& t, int vb, uint4 (&cur)[kPer]) {
-    const bool ok = wait(l, &l.full[t.st], t.ph);
-    const uint4* st = ring + t.st * kChunk + threadIdx.x;
-    if (s.inner(vb)) {
+// One pass over the slice: many(cur, vb) takes this thread's vectors of a chunk
+// that lies wholly in the slice, vector vb + thread + u kNT being cur[u];
+// one(w, v, vb) takes vector v of another chunk (-inf past the slice's end, called
+// by warps with any vector in it); after(n) follows the n-th chunk.  False once a
+// wait ran out.
+template <int DT, class Many, class One, class After>
+__device__ __forceinline__ bool consume(const Slice<DT>& s, const uint4* ring, Link& l, Turn& t, Many many, One one,
+                                        After after) {
+    bool ok = true;
+    int n = 0;
+    for (int vb = s.v0; vb < s.v1; vb += kChunk) {
+        ok &= wait(l, &l.full[t.st], t.ph);
+        const uint4* st = ring + t.st * kChunk + threadIdx.x;
+        if (s.inner(vb)) {
+            uint4 cur[kPer];
 #pragma unroll
-        for (int u = 0; u < kPer; ++u) cur[u] = st[u * kNT];
-    } else {
-#pragma unroll
-        for (int u = 0; u < kPer; ++u) {
-            const int v = vb + threadIdx.x + u * kNT;
-            if (v >= s.f0 && v < s.f1 && v < s.v1) cur[u] = st[u * kNT];
-            else if (v < s.v1) cur[u] = s.row.load_edge((int64_t)v * El<DT>::E - s.row.mis);
-            else cur[u] = make_uint4(El<DT>::ninf, El<DT>::ninf, El<DT>::ninf, El<DT>::ninf);
+            for (int u = 0; u < kPer; ++u) cur[u] = st[u * kNT];
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) u_mb_arrive(&l.empty[t.st]);
+            many(cur, vb);
+        } else {
+            const int end = min(s.f1, s.v1), warp = threadIdx.x & ~31;
+#pragma unroll 1
+            for (int u = 0; u < kPer && vb + warp + u * kNT < s.v1; ++u) {
+                const int v = vb + threadIdx.x + u * kNT;
+                uint4 w[1] = {make_uint4(El<DT>::ninf, El<DT>::ninf, El<DT>::ninf, El<DT>::ninf)};
+                if (v >= s.f0 && v < end) w[0] = st[u * kNT];
+                else if (v < s.v1) w[0] = s.row.load_edge((int64_t)v * El<DT>::E - s.row.mis);
+                one(w, v, vb);
+            }
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) u_mb_arrive(&l.empty[t.st]);
         }
+        t.step();
+        after(++n);
     }
-    __syncwarp();
-    if ((threadIdx.x & 31) == 0) u_mb_arrive(&l.empty[t.st]);
-    t.step();
     return ok;
 }
 
-// The row's joined softmax from the threads' and, in a cluster, the CTAs'.
-// turn: the row's number; *cta: the CTA's own.
 template <int DT>
 __device__ __forceinline__ Run join_warps(const float4* w, int n, float c) {
     float m = -kInf;
@@ -543,11 +590,16 @@ __device__ __forceinline__ Run join_warps(const float4* w, int n, float c) {
     }
     return r;
 }
+// The row's joined softmax from the threads' and, in a cluster, the CTAs'.
+// turn: the row's number; *top (may be null): becomes the CTA's largest.
 template <int DT>
-__device__ __forceinline__ Run row_reduce(Run r, Link& l, float c, int turn, int rank, int cs, Run* cta) {
-    float m = r.m;
+__device__ __forceinline__ Run row_reduce(Run r, Link& l, float c, int turn, int rank, int cs, float* top) {
+    float m = r.m, t = top ? *top : 0.f;
 #pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
+    for (int o = 16; o; o >>= 1) {
+        m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
+        if (top) t = fmaxf(t, __shfl_xor_sync(kFull, t, o));
+    }
     if (r.m != m) run_to<DT>(r, m, c);
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
@@ -555,10 +607,11 @@ __device__ __forceinline__ Run row_reduce(Run r, Link& l, float c, int turn, int
         r.a += __shfl_xor_sync(kFull, r.a, o);
     }
     const int p = turn & 1;
-    if ((threadIdx.x & 31) == 0) l.warp[p][threadIdx.x >> 5] = make_float4(m, r.s, r.a, 0.f);
+    if ((threadIdx.x & 31) == 0) l.warp[p][threadIdx.x >> 5] = make_float4(m, r.s, r.a, t);
     consumers_sync();
     r = join_warps<DT>(l.warp[p], kWarps, c);
-    *cta = r;
+    if (top)
+        for (int i = 0; i < kWarps; ++i) *top = fmaxf(*top, l.warp[p][i].w);
     if (cs > 1) {
         if (threadIdx.x < cs) {
             cg::cluster_group cl = cg::this_cluster();
@@ -737,77 +790,60 @@ __device__ __noinline__ int recollect(const Row<DT>& row, int v0, int v1, int k,
     return n;
 }
 
-// A bound that at least k of the groups' maxima reach (16-bit orders, two per
-// word of g; empty groups are 0), and few more: four candidates are counted per
-// barrier, first in growing steps below the slice's maximum, then between the
-// last that too few reached and the first that enough did.
-__device__ unsigned group_bound(const uint32_t (&g)[kMaxGroups / 2], unsigned top, int k, TopShared& ts, int& turn) {
-    const int few = k + k / 4 + 16;
-    int lo = 1, hi = (int)top + 1;  // enough reach lo (or there are not that many), too few reach hi
-    int at_lo = 1 << 30;
+// A bound that at least k of the threads' marks reach, and few more: four
+// candidates are counted per barrier, first in growing steps below the largest
+// value's order, then between the last that too few reached and the first that
+// enough did.
+__device__ unsigned mark_bound(int mark, int top, int k, TopShared& ts, int& turn) {
+    constexpr int kNone = 1 << 30;
+    const int few = k + k / 8 + 8;
+    int lo = 1, hi = top + 1, at_lo = kNone;  // at_lo marks reach lo; too few reach hi
     for (int step = 4; at_lo > few && hi - lo > 1;) {
         int c[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            c[i] = at_lo == 1 << 30 ? max(lo, (int)top - (step << (2 * i))) : lo + (int)((int64_t)(hi - lo) * (4 - i) / 5);
-        int n01 = 0, n23 = 0;
-#pragma unroll
-        for (int j = 0; j < kMaxGroups / 2; ++j) {
-            const int a = (int)(g[j] & 0xffffu), b = (int)(g[j] >> 16);
-            n01 += (a >= c[0]) + (b >= c[0]) + (((a >= c[1]) + (b >= c[1])) << 16);
-            n23 += (a >= c[2]) + (b >= c[2]) + (((a >= c[3]) + (b >= c[3])) << 16);
-        }
-        const int2 s = block_sum(n01, n23, ts, turn);
+        for (int i = 0; i < 4; ++i) c[i] = at_lo == kNone ? max(lo, top - (step << (2 * i))) : lo + (hi - lo) * (4 - i) / 5;
+        const int2 s = block_sum((mark >= c[0]) + ((mark >= c[1]) << 16), (mark >= c[2]) + ((mark >= c[3]) << 16), ts, turn);
         const int n[4] = {s.x & 0xffff, (int)((unsigned)s.x >> 16), s.y & 0xffff, (int)((unsigned)s.y >> 16)};
         int found = 4;
 #pragma unroll
         for (int i = 3; i >= 0; --i)
             if (n[i] >= k) found = i;
         if (found == 4) {
-            if (at_lo != 1 << 30 || c[3] > lo) hi = c[3];
-            else at_lo = 0;  // fewer than k groups at all: every one counts
+            if (at_lo == kNone && c[3] == lo) at_lo = 0;  // fewer than k marks: all of them count
+            hi = c[3];
             step <<= 8;
         } else {
-            if (found) hi = c[0];
 #pragma unroll
-            for (int i = 1; i < 4; ++i)
-                if (found > i) hi = c[i];
-            lo = c[0];
-            at_lo = n[0];
-#pragma unroll
-            for (int i = 1; i < 4; ++i)
-                if (found == i) lo = c[i], at_lo = n[i];
+            for (int i = 0; i < 4; ++i) {
+                if (i < found) hi = c[i];
+                if (i == found) lo = c[i], at_lo = n[i];
+            }
         }
     }
     return (unsigned)lo;
 }
 
-// The best k tokens of a slice, given the maxima of its groups (ts.group) and its
-// largest value: a bound that at least k group maxima reach bounds the k-th best
-// element from below, and only the groups that reach it (k and a few) are read
-// again, from L2.  Group j of thread t: its vectors of chunks [j per, (j + 1) per).
-// Returns how many are in ts.best.
+// The best k tokens of a slice.  mark: upper half of the order of the largest of
+// this thread's elements; top: the slice's largest value.  A bound that at least k
+// threads' marks reach bounds the k-th best element from below, and nearly as
+// tightly as the k-th best itself, as the best rarely share a thread.  Only the
+// groups of vectors whose maxima (ts.group) reach it, k and a few, are read
+// again, from L2.  Group j of thread t: its vectors of chunks [j per, (j + 1)
+// per).  Returns how many are in ts.best.
 template <int DT>
-__device__ int slice_best(const Slice<DT>& s, int groups, int per, float top, int k, TopShared& ts, int& turn) {
+__device__ int slice_best(const Slice<DT>& s, int groups, int per, unsigned mark, float top, int k, TopShared& ts, int& turn) {
     constexpr int E = El<DT>::E;
     const int tid = threadIdx.x;
-    uint32_t g[kMaxGroups / 2];  // this thread's maxima, in pairs
-#pragma unroll
-    for (int j = 0; j < kMaxGroups / 2; ++j) {
-        g[j] = 0;
-        if (2 * j < groups) g[j] = ts.group[2 * j * kNT + tid];
-        if (2 * j + 1 < groups) g[j] |= (uint32_t)ts.group[(2 * j + 1) * kNT + tid] << 16;
-    }
-    const unsigned P = group_bound(g, order_of(top) >> 16, k, ts, turn);
+    const unsigned P = mark_bound((int)mark, (int)(order_of(top) >> 16), k, ts, turn);
     // the lowest value of that order; nothing but -inf lies below the first
     const float thr = P <= 0x7fu ? -FLT_MAX : value_of(P << 16);
     const unsigned least = max(P, order_of(-FLT_MAX) >> 16);
-#pragma unroll
-    for (int j = 0; j < kMaxGroups; ++j)
-        if ((g[j / 2] >> (16 * (j & 1)) & 0xffffu) >= least) {
-            const int at = atomicAdd(&ts.n_hits, 1);
-            if (at < kMaxHits) ts.list[at] = j * kNT + tid;
-        }
+    if (mark >= least)
+        for (int j = 0; j < groups; ++j)
+            if (ts.group[j * kNT + tid] >= least) {
+                const int at = atomicAdd(&ts.n_hits, 1);
+                if (at < kMaxHits) ts.list[at] = j * kNT + tid;
+            }
     consumers_sync();
     const int hits = ts.n_hits;
     int n = kCand + 1;
@@ -868,26 +904,32 @@ __global__ void __launch_bounds__(kThreads, 2) k_logprobs(LogprobArgs a, int cs)
             const Slice<DT> s(a.logits, a.ld, r, a.vocab, rank, cs);
             const int chunks = s.chunks(), per = (chunks + kMaxGroups - 1) / kMaxGroups;
             Acc<DT, true> acc;
-            int group = 0, in_group = 0;
-            float gm = -kInf;
-            bool ok = true;
+            int group = 0;
+            float gm = -kInf, top = -kInf;  // largest of the group, of this thread's vectors
             if (TOP && tid == 0) ts.n = ts.n_hits = 0;
-            for (int b = 0; b < chunks; ++b) {
-                uint4 cur[kPer];
-                ok &= fetch(s, ring, l, at, s.v0 + b * kChunk, cur);
-                const float vm = max_of<DT>(cur);
-                acc.add(cur, vm, c);
-                if (TOP) gm = max_nan(gm, vm);
-                if (TOP && (++in_group == per || b + 1 == chunks)) {
-                    ts.group[group * kNT + tid] = (uint16_t)(order_of(gm) >> 16);
-                    ++group;
-                    in_group = 0;
-                    gm = -kInf;
-                }
-            }
-            Run mine = acc.get(), cta;
+            const bool ok = consume(
+                s, ring, l, at,
+                [&](uint4(&cur)[kPer], int) {
+                    const float vm = max_of<DT>(cur);
+                    acc.add(cur, vm, c);
+                    if (TOP) gm = max_nan(gm, vm);
+                },
+                [&](uint4(&w)[1], int, int) {
+                    const float vm = El<DT>::vmax(w[0]);
+                    acc.add(w, vm, c);
+                    if (TOP) gm = max_nan(gm, vm);
+                },
+                [&](int n) {
+                    if (TOP && (n == (group + 1) * per || n == chunks)) {
+                        ts.group[group++ * kNT + tid] = (uint16_t)(order_of(gm) >> 16);
+                        top = max_nan(top, gm);
+                        gm = -kInf;
+                    }
+                });
+            Run mine = acc.get();
             if (!ok) mine.s = kNan;
-            const Run run = row_reduce<DT>(mine, l, c, i, rank, cs, &cta);
+            const unsigned mark = order_of(top) >> 16;
+            const Run run = row_reduce<DT>(mine, l, c, i, rank, cs, TOP ? &top : nullptr);
             const bool none = run.m == -kInf && run.s == 0.f;
             const float lns = log_sum<DT>(run.s, run.m, c);
             if (rank == 0 && tid == 0) {
@@ -902,7 +944,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_logprobs(LogprobArgs a, int cs)
                 }
             }
             if constexpr (TOP) {
-                int nb = slice_best<DT>(s, group, per, cta.m, a.k, ts, turn);
+                int nb = slice_best<DT>(s, group, per, mark, top, a.k, ts, turn);
                 if (cs > 1) {
                     if (rank) {  // to the first CTA, which is past the row before once this row's sums are exchanged
                         TopShared* o = cg::this_cluster().map_shared_rank(&ts, 0);
@@ -989,11 +1031,11 @@ struct DistillArgs {
 struct ListShared {
     double q[kMaxList], c;  // weights; sum of q (log q - x / T)
     double sum, inv_t;      // sum of q
-    int id[kMaxList];       // -1: absent
+    alignas(16) int id[kMaxList];  // -1: absent
     float x[kMaxList];      // the row's value there
     float t[kMaxList];      // the teacher's value
     float merged[kMaxList]; // weight of the token, all its entries together
-    int next[kMaxList];     // -1 where an earlier entry names this token, else the entry itself
+    int next[kMaxList];     // -1: absent or named by an earlier entry; else how many later ones name it
     float q0, m, s;         // what the list leaves over; largest x, sum of powers relative to it
 };
 
@@ -1025,6 +1067,7 @@ __device__ __forceinline__ void list_read(const DistillArgs& a, const Row<DT>& r
         ls.t[i] = in ? t : -kInf;
         ls.x[i] = in ? El<DT>::one(row.p[id]) : -kInf;
     }
+    if (lane < 4 && a.k + lane < kMaxList) ls.id[a.k + lane] = -2;  // (read in fours)
 }
 
 // What follows from the list by itself (one warp).  The weights and the loss's
@@ -1046,9 +1089,16 @@ __device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls) {
     int listed = 0;
     for (int i = lane; i < a.k; i += 32) {
         const int id = ls.id[i];
-        bool first = id >= 0;
-        for (int j = 0; j < i && first; ++j) first = ls.id[j] != id;
-        ls.next[i] = first ? i : -1;
+        int before = 0, after = 0;  // other entries of the same token
+        const int4* all = reinterpret_cast<const int4*>(ls.id);
+#pragma unroll 4
+        for (int j = 0; j < a.k; j += 4) {
+            const int4 o = all[j >> 2];
+            before += (j < i && o.x == id) + (j + 1 < i && o.y == id) + (j + 2 < i && o.z == id) + (j + 3 < i && o.w == id);
+            after += (j > i && o.x == id) + (j + 1 > i && o.y == id) + (j + 2 > i && o.z == id) + (j + 3 > i && o.w == id);
+        }
+        const bool first = id >= 0 && before == 0;
+        ls.next[i] = first ? after : -1;
         listed += first;
         if (first) s += ex2(exponent<DT>(ls.x[i], m, c));
         const double e = exp((double)ls.t[i] - tm);
@@ -1069,9 +1119,9 @@ __device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls) {
     part = warp_sum(part);
     __syncwarp();
     for (int i = lane; i < a.k; i += 32) {
-        double q = 0.0;
-        if (ls.next[i] >= 0)
-            for (int j = i; j < a.k; ++j)
+        double q = ls.q[i];
+        if (ls.next[i] > 0)
+            for (int j = i + 1; j < a.k; ++j)
                 if (ls.id[j] == ls.id[i]) q += ls.q[j];
         ls.merged[i] = (float)q;
     }
@@ -1181,17 +1231,6 @@ struct GradRow {
     }
 };
 
-// The vector with the elements of mask m out of the way.
-template <int DT>
-__device__ __noinline__ uint4 without(uint4 v, uint32_t m) {
-    float x[El<DT>::E];
-    El<DT>::unpack(v, x);
-#pragma unroll
-    for (int e = 0; e < El<DT>::E; ++e)
-        if (m >> e & 1) x[e] = -kInf;
-    return El<DT>::pack(x);  // (what came from this type goes back unrounded)
-}
-
 // Loss, statistics for a later backward pass and (GRAD) the gradient.  The
 // gradient's second read of a row comes from L2: the rows in flight fit there
 // (cluster_size).
@@ -1249,23 +1288,31 @@ __global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) 
             }
             consumers_sync();
             Acc<DT, false> acc;
-            for (int vb = s.v0, b = 0; vb < s.v1; vb += kChunk, ++b) {
-                uint4 cur[kPer];
-                ok &= fetch(s, ring, l, at, vb, cur);
-                const uint32_t here = flags[b * kWarps + (tid >> 5)];  // (alike for the warp)
-                if (here) {
+            // the listed elements of vector v out of the way
+            auto mask = [&](uint4& w, int v) {
+                const int e = (v - s.v0) * E;
+                const uint32_t m = bits[e >> 5] >> (e & 31) & ((1u << E) - 1);
+                if (m) w = El<DT>::without(w, m);
+            };
+            ok &= consume(
+                s, ring, l, at,
+                [&](uint4(&cur)[kPer], int vb) {
+                    const uint32_t here = flags[(vb - s.v0) / kChunk * kWarps + (tid >> 5)];  // (alike for the warp)
+                    if (here) {
 #pragma unroll
-                    for (int u = 0; u < kPer; ++u)
-                        if (here >> u & 1) {
-                            const int e = (vb - s.v0 + tid + u * kNT) * E;
-                            if (e < (s.v1 - s.v0) * E) cur[u] = without<DT>(cur[u], bits[e >> 5] >> (e & 31) & ((1u << E) - 1));
-                        }
-                }
-                acc.add(cur, max_of<DT>(cur), c);
-            }
-            Run run = acc.get(), cta;
+                        for (int u = 0; u < kPer; ++u)
+                            if (here >> u & 1) mask(cur[u], vb + tid + u * kNT);
+                    }
+                    acc.add(cur, max_of<DT>(cur), c);
+                },
+                [&](uint4(&w)[1], int v, int) {
+                    if (v < s.v1) mask(w[0], v);
+                    acc.add(w, El<DT>::vmax(w[0]), c);
+                },
+                [](int) {});
+            Run run = acc.get();
             if (!ok) run.s = kNan;
-            run = row_reduce<DT>(run, l, c, i, rank, cs, &cta);
+            run = row_reduce<DT>(run, l, c, i, rank, cs, nullptr);
             if (bit >= 0) bits[bit >> 5] = flags[flag] = 0;  // (all are past the row; the next one's are set after the barrier below)
             float loss;
             const float4 coef = row_finish<DT>(a, run, c, ls, rank == 0 && tid == 0 ? &loss : nullptr);
@@ -1280,25 +1327,24 @@ __global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) 
                     for (int v = s.v0 + tid; v < s.v1; v += kNT) out.put(s.row, v, make_uint4(0, 0, 0, 0));
                 } else {
                     const GradOf<DT> grad(coef, c, f);
-                    for (int vb = s.v0; vb < s.v1; vb += kChunk) {
-                        uint4 cur[kPer];
-                        ok &= fetch(s, ring, l, at, vb, cur);
-                        if (s.inner(vb) && out.aligned && ok) {
-                            uint4* to = reinterpret_cast<uint4*>(out.g + ((int64_t)(vb + tid) * E - s.row.mis));
+                    ok &= consume(
+                        s, ring, l, at,
+                        [&](uint4(&cur)[kPer], int vb) {
+                            if (out.aligned) {
+                                uint4* to = reinterpret_cast<uint4*>(out.g + ((int64_t)(vb + tid) * E - s.row.mis));
 #pragma unroll
-                            for (int u = 0; u < kPer; ++u) __stcs(to + u * kNT, grad(cur[u]));
-                        } else {
-#pragma unroll 1
-                            for (int u = 0; u < kPer; ++u) {
-                                const int v = vb + tid + u * kNT;
-                                uint4 w4 = cur[0];
+                                for (int u = 0; u < kPer; ++u) __stcs(to + u * kNT, grad(cur[u]));
+                            } else {
 #pragma unroll
-                                for (int j = 1; j < kPer; ++j) w4 = u == j ? cur[j] : w4;
-                                w4 = ok ? grad(w4) : make_uint4(kFull, kFull, kFull, kFull);  // NaN in every type
-                                if (v < s.v1) out.put(s.row, v, w4);
+                                for (int u = 0; u < kPer; ++u) out.put(s.row, vb + tid + u * kNT, grad(cur[u]));
                             }
-                        }
-                    }
+                        },
+                        [&](uint4(&x)[1], int v, int) {
+                            if (v < s.v1) out.put(s.row, v, grad(x[0]));
+                        },
+                        [](int) {});
+                    if (!ok)  // NaN in every type
+                        for (int v = s.v0 + tid; v < s.v1; v += kNT) out.put(s.row, v, make_uint4(kFull, kFull, kFull, kFull));
                 }
                 consumers_sync();
                 if (w != 0.f && ok) out.listed(a, s.row, s.v0, s.v1, c, f, coef, ls, kNT);
