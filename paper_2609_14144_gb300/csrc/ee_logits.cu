@@ -12,6 +12,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 #include <float.h>
+#include <stddef.h>
 #include <stdint.h>
 
 #include <algorithm>
@@ -405,12 +406,13 @@ struct Acc {
 // number of instructions per element (a budget of about 11 per element of two
 // bytes): a chunk that lies wholly in the slice has one wait, one comparison and
 // no other condition.
-constexpr int kNT = 384;                 // consuming threads
+constexpr int kNT = 256;                 // consuming threads
 constexpr int kWarps = kNT / 32;
 constexpr int kThreads = kNT + 64;
 constexpr int kPer = 4;                  // vectors per thread and chunk
-constexpr int kChunk = kNT * kPer;       // vectors per stage: 24 KB
+constexpr int kChunk = kNT * kPer;       // vectors per stage: 16 KB
 constexpr int kStages = 3;
+constexpr int kCtas = 3;                 // that fit an SM
 constexpr int kRingBytes = kStages * kChunk * 16;
 
 // Words of a slice's listed bits and of the flags over them.
@@ -420,8 +422,11 @@ __host__ __device__ inline int slice_flags(int vocab, int E, int cs) {
     return (slice_vecs(vocab, E, cs) + kChunk - 1) / kChunk * kWarps;
 }
 
-__device__ __forceinline__ void consumers_sync() { asm volatile("bar.sync 1, 384;" ::: "memory"); }
-static_assert(kNT == 384, "consumers_sync");
+__device__ __forceinline__ void consumers_sync() {
+    __syncwarp();  // (the barrier counts a warp as a whole)
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+}
+static_assert(kNT == 256, "consumers_sync");
 
 // m: largest value so far (-inf: none); s: sum of 2^t; a: sum of t 2^t.
 struct Link {
@@ -537,6 +542,16 @@ __device__ void drain(Link& l, Turn t, int64_t n) {
     }
 }
 
+// This warp has read its part of the stage.  The proxy fence comes first: the
+// reads have to be done before the stage's next bulk copy may be issued, and
+// without it loads that queued behind a burst of stores were overtaken by the
+// arrival (a row's gradient then held powers of the chunk three further on).
+__device__ __forceinline__ void release(Link& l, const Turn& t) {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) u_mb_arrive(&l.empty[t.st]);
+}
+
 // One pass over the slice: many(cur, vb) takes this thread's vectors of a chunk
 // that lies wholly in the slice, vector vb + thread + u kNT being cur[u];
 // one(w, v, vb) takes vector v of another chunk (-inf past the slice's end, called
@@ -554,8 +569,7 @@ __device__ __forceinline__ bool consume(const Slice<DT>& s, const uint4* ring, L
             uint4 cur[kPer];
 #pragma unroll
             for (int u = 0; u < kPer; ++u) cur[u] = st[u * kNT];
-            __syncwarp();
-            if ((threadIdx.x & 31) == 0) u_mb_arrive(&l.empty[t.st]);
+            release(l, t);
             many(cur, vb);
         } else {
             const int end = min(s.f1, s.v1), warp = threadIdx.x & ~31;
@@ -567,8 +581,7 @@ __device__ __forceinline__ bool consume(const Slice<DT>& s, const uint4* ring, L
                 else if (v < s.v1) w[0] = s.row.load_edge((int64_t)v * El<DT>::E - s.row.mis);
                 one(w, v, vb);
             }
-            __syncwarp();
-            if ((threadIdx.x & 31) == 0) u_mb_arrive(&l.empty[t.st]);
+            release(l, t);
         }
         t.step();
         after(++n);
@@ -576,17 +589,20 @@ __device__ __forceinline__ bool consume(const Slice<DT>& s, const uint4* ring, L
     return ok;
 }
 
+// Joins n <= 16 states; every lane returns the result.
 template <int DT>
-__device__ __forceinline__ Run join_warps(const float4* w, int n, float c) {
-    float m = -kInf;
-    for (int i = 0; i < n; ++i) m = fmaxf(m, w[i].x);
-    Run r{m, 0.f, 0.f};
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-        Run o{w[i].x, w[i].y, w[i].z};
-        if (o.m != m) run_to<DT>(o, m, c);
-        r.s += o.s;
-        r.a += o.a;
+__device__ __forceinline__ Run join_states(const float4* w, int n, float c) {
+    const int i = threadIdx.x & 15;
+    Run r{-kInf, 0.f, 0.f};
+    if (i < n) r = Run{w[i].x, w[i].y, w[i].z};
+    float m = r.m;
+#pragma unroll
+    for (int o = 8; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kFull, m, o));
+    if (r.m != m) run_to<DT>(r, m, c);
+#pragma unroll
+    for (int o = 8; o; o >>= 1) {
+        r.s += __shfl_xor_sync(kFull, r.s, o);
+        r.a += __shfl_xor_sync(kFull, r.a, o);
     }
     return r;
 }
@@ -609,7 +625,7 @@ __device__ __forceinline__ Run row_reduce(Run r, Link& l, float c, int turn, int
     const int p = turn & 1;
     if ((threadIdx.x & 31) == 0) l.warp[p][threadIdx.x >> 5] = make_float4(m, r.s, r.a, t);
     consumers_sync();
-    r = join_warps<DT>(l.warp[p], kWarps, c);
+    r = join_states<DT>(l.warp[p], kWarps, c);
     if (top)
         for (int i = 0; i < kWarps; ++i) *top = fmaxf(*top, l.warp[p][i].w);
     if (cs > 1) {
@@ -619,7 +635,7 @@ __device__ __forceinline__ Run row_reduce(Run r, Link& l, float c, int turn, int
             arrive_at(&l.exchange, threadIdx.x);
         }
         const bool ok = wait(l, &l.exchange, p);
-        r = join_warps<DT>(l.peer[p], cs, c);
+        r = join_states<DT>(l.peer[p], cs, c);
         if (!ok) r.s = kNan;
     }
     return r;
@@ -652,7 +668,6 @@ struct TopShared {
     unsigned long long keys[kCand];
     unsigned long long best[kMaxList];
     unsigned long long surv[kEnough];
-    unsigned long long join[(kMaxCluster - 1) * kMaxList];  // the first CTA's: the others' best
     uint16_t group[kMaxGroups * kNT];  // upper half of the order of each group's maximum
     unsigned hist[256];
     int list[kMaxHits];  // groups that may hold one of the best
@@ -663,6 +678,7 @@ struct TopShared {
     int2 sum[3];   // rotating counters of block_sum, zero between uses
     unsigned long long prefix;
     int done;
+    unsigned long long join[(kMaxCluster - 1) * kMaxList];  // the first CTA's, in clusters alone: the others' best
 };
 
 // Two sums over the consumers with one barrier: a slot is cleared two calls
@@ -738,7 +754,7 @@ __device__ __noinline__ int recollect(const Row<DT>& row, int v0, int v1, int k,
     unsigned long long prefix = 0;
     int above = 0;  // keys known to lie above the prefix
     for (int shift = 56;; shift -= 8) {
-        if (threadIdx.x < 256) sh.hist[threadIdx.x] = 0;
+        sh.hist[threadIdx.x] = 0;
         consumers_sync();
         for (int vb = v0; vb < v1; vb += kNT) {
             const int v = vb + threadIdx.x;
@@ -881,7 +897,7 @@ struct LogprobArgs {
 // For the best tokens the pass keeps the maximum of every group of vectors, which
 // the running softmax needs anyway; slice_best does the rest.
 template <int DT, bool TOP>
-__global__ void __launch_bounds__(kThreads, 2) k_logprobs(LogprobArgs a, int cs) {
+__global__ void __launch_bounds__(kThreads, kCtas) k_logprobs(LogprobArgs a, int cs) {
     extern __shared__ __align__(128) uint8_t l_smem[];
     uint4* ring = reinterpret_cast<uint4*>(l_smem);
     Link& l = *reinterpret_cast<Link*>(l_smem + kRingBytes);
@@ -1429,24 +1445,24 @@ int check_logits(const void* p, int type, int64_t rows, int vocab, int64_t ld, f
 // by a cluster, as long as every CTA keeps a stage of vectors.  A pass that reads
 // its rows twice shares them until the rows in flight fit in L2 beside what it
 // writes.
-int cluster_size(int64_t rows, int vocab, int type, int n_sm, bool twice) {
+int cluster_size(int64_t rows, int vocab, int type, int n_sm, int ctas, bool twice) {
     const int64_t bytes = (int64_t)vocab * (int64_t)elem_bytes(type), vecs = bytes / 16;
     int cs = 1;
     while (cs < kMaxCluster &&
            ((vecs / (2 * cs) >= kChunk &&
-             (rows * cs < n_sm || (twice && bytes * std::min<int64_t>(rows, 2 * n_sm / cs) > kL2Rows))) ||
+             (rows * cs < n_sm || (twice && bytes * std::min<int64_t>(rows, ctas * n_sm / cs) > kL2Rows))) ||
             vocab / cs > kMaxSlice))
         cs *= 2;
     return cs;
 }
 
 template <class K, class A>
-int launch_rows(K kern, int64_t rows, int cs, int n_sm, size_t smem, cudaStream_t s, const A& args) {
+int launch_rows(K kern, int64_t rows, int cs, int ctas, size_t smem, cudaStream_t s, const A& args) {
     // (one limit for every size: calls of other threads may set it too)
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
     if (e != cudaSuccess) return cuda_status(e);
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(std::min<int64_t>(rows, std::max(1, 2 * n_sm / cs)) * cs));
+    cfg.gridDim = dim3((unsigned)(std::min<int64_t>(rows, std::max(1, ctas / cs)) * cs));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
@@ -1462,15 +1478,15 @@ int launch_rows(K kern, int64_t rows, int cs, int n_sm, size_t smem, cudaStream_
 template <int DT>
 int run_logprobs(const LogprobArgs& a, int cs, int n_sm, cudaStream_t s) {
     const size_t smem = kRingBytes + sizeof(Link);
-    return a.k ? launch_rows(k_logprobs<DT, true>, a.rows, cs, n_sm, smem + sizeof(TopShared), s, a)
-               : launch_rows(k_logprobs<DT, false>, a.rows, cs, n_sm, smem, s, a);
+    return a.k ? launch_rows(k_logprobs<DT, true>, a.rows, cs, kCtas * n_sm, smem + (cs > 1 ? sizeof(TopShared) : offsetof(TopShared, join)), s, a)
+               : launch_rows(k_logprobs<DT, false>, a.rows, cs, kCtas * n_sm, smem, s, a);
 }
 
 template <int DT>
 int run_distill(const DistillArgs& a, int cs, int n_sm, cudaStream_t s) {
     const size_t smem = kRingBytes + sizeof(Link) + 2 * sizeof(ListShared) + 4 * (size_t)(slice_flags(a.vocab, El<DT>::E, cs) + slice_words(a.vocab, El<DT>::E, cs));
-    return a.grad ? launch_rows(k_distill<DT, true>, a.rows, cs, n_sm, smem, s, a)
-                  : launch_rows(k_distill<DT, false>, a.rows, cs, n_sm, smem, s, a);
+    return a.grad ? launch_rows(k_distill<DT, true>, a.rows, cs, 2 * n_sm, smem, s, a)
+                  : launch_rows(k_distill<DT, false>, a.rows, cs, 2 * n_sm, smem, s, a);
 }
 
 int check_list(const int32_t* ids, int64_t ld_ids, const float* teacher, int64_t ld_teacher, int k, int64_t rows) {
@@ -1504,7 +1520,7 @@ int ee_token_logprobs(const void* logits, int type, int64_t rows, int vocab, int
     int n_sm = 0;
     if ((rc = sm_count(&n_sm)) != EE_OK) return rc;
     const LogprobArgs a{logits, ld, rows, vocab, k, ids, temperature, logprob, entropy, lse, top_logprob, top_id};
-    const int cs = cluster_size(rows, vocab, type, n_sm, false);
+    const int cs = cluster_size(rows, vocab, type, n_sm, kCtas, false);
     cudaStream_t s = (cudaStream_t)stream;
     if (type == EE_BF16) return run_logprobs<EE_BF16>(a, cs, n_sm, s);
     if (type == EE_FP16) return run_logprobs<EE_FP16>(a, cs, n_sm, s);
@@ -1523,7 +1539,7 @@ int ee_distill_topk(const void* logits, int type, int64_t rows, int vocab, int64
     if ((uintptr_t)stats % 16) return fail(EE_EINVAL, "stats must be 16-byte aligned");
     int n_sm = 0;
     if ((rc = sm_count(&n_sm)) != EE_OK) return rc;
-    const int cs = cluster_size(rows, vocab, type, n_sm, grad != nullptr);
+    const int cs = cluster_size(rows, vocab, type, n_sm, 2, grad != nullptr);
     const DistillArgs a{logits, ld, rows, vocab, k, tail ? 1 : 0, ids, ld_ids, teacher, ld_teacher, temperature, weight, loss,
                         reinterpret_cast<float4*>(stats), grad, ld_grad};
     cudaStream_t s = (cudaStream_t)stream;

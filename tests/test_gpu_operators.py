@@ -520,6 +520,20 @@ def test_distill_special_rows(rows, V, tail):
     assert loss.shape == (0,) and grad.shape == (0, V)
 
 
+def test_distill_rows_whose_writes_lag_behind_their_reads():
+    """Rows of the gradient off the 16-byte grid of the logits' are written element
+    by element, so that the shared-memory ring runs full behind a queue of stores:
+    every call gives the same bits as the backward pass, which has no ring."""
+    g = gen(21)
+    z = normal(g, 2, 400000, BF16, 3.0, 1, 5)
+    ids, t = teacher_list(g, z, 3, 1.0, True)
+    w = torch.ones(2, device="cuda")
+    _, stats = ee.distill_topk(z, ids, t, tail=True)
+    want = ee.distill_topk_backward(w, z, ids, t, stats, tail=True)
+    for i in range(200):
+        assert torch.equal(ee.distill_topk_step(z, ids, t, w, tail=True)[1], want), i
+
+
 def test_results_do_not_change_from_call_to_call():
     g = gen(12)
     z = normal(g, 40, 50257, BF16, 3.0)
