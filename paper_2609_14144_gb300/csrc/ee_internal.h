@@ -344,4 +344,7 @@ inline int64_t tiled_elems(int64_t rows, int64_t K) { return tile_count(rows) * 
 // or null.
 void* tensor_map_encoder();
 
+// out [d] = sum of n rows of part [n][d], in a fixed order (ee_norm.cu).
+cudaError_t launch_sum_parts(const float* part, int n, int d, float* out, cudaStream_t s);
+
 }  // namespace ee

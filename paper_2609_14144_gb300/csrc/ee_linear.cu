@@ -176,8 +176,20 @@ __device__ __forceinline__ void emit8x4(const Epilogue& e, int64_t row0, int64_t
 }
 
 // ---------------------------------------------------------------- few rows
+__device__ __forceinline__ void unpack8(const uint4& v, int type, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpack2(w[i], type);
+        x[2 * i] = f.x, x[2 * i + 1] = f.y;
+    }
+}
+
 // R rows (rows past `rows` repeat the last one and are not written), WN outputs
-// per warp; a lane takes 8 columns of every 256.
+// per warp (likewise).  VEC: a lane takes 8 columns of every 256, n_in being a
+// multiple of 8; all loads of a step go out before its first product (a bounds
+// test around each made them wait for one another: 16 us instead of 5.3 for one row
+// of 896 and 4864 outputs).  Otherwise a lane takes every 32nd column.
 template <int R, int WN, bool VEC>
 __global__ void __launch_bounds__(128) k_linear_few(const uint16_t* __restrict__ x, int64_t ld_x, int rows,
                                                     const uint16_t* __restrict__ w, int64_t ld_w, int n_in, int n_out,
@@ -186,26 +198,57 @@ __global__ void __launch_bounds__(128) k_linear_few(const uint16_t* __restrict__
     const int o0 = (blockIdx.x * 4 + (threadIdx.x >> 5)) * WN;
     if (o0 >= n_out) return;
     float acc[WN][R];
+    const uint16_t *wp[WN], *xp[R];
 #pragma unroll
-    for (int i = 0; i < WN; ++i)
+    for (int i = 0; i < WN; ++i) {
+        wp[i] = w + (int64_t)(o0 + i < n_out ? o0 + i : n_out - 1) * ld_w;
 #pragma unroll
         for (int r = 0; r < R; ++r) acc[i][r] = 0.f;
-#pragma unroll 2
-    for (int c = lane * 8; c < n_in; c += 256) {
-        float wv[WN][8];
+    }
 #pragma unroll
-        for (int i = 0; i < WN; ++i) {
-            const int o = o0 + i < n_out ? o0 + i : n_out - 1;
-            load8(w + o * ld_w + c, e.type, n_in - c, VEC, wv[i]);
+    for (int r = 0; r < R; ++r) xp[r] = x + (r < rows ? r : rows - 1) * ld_x;
+    if (VEC) {
+        // steps whose loads are in flight together
+        constexpr int U = WN * R >= 16 ? 1 : WN * R >= 4 ? 2 : 4;
+        for (int c0 = lane * 8; c0 < n_in; c0 += 256 * U) {
+            uint4 wv[U][WN], xv[U][R];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c0 + 256 * u < n_in) {
+#pragma unroll
+                    for (int i = 0; i < WN; ++i) wv[u][i] = __ldg((const uint4*)(wp[i] + c0 + 256 * u));
+#pragma unroll
+                    for (int r = 0; r < R; ++r) xv[u][r] = __ldg((const uint4*)(xp[r] + c0 + 256 * u));
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c0 + 256 * u < n_in) {
+                    float f[WN][8];
+#pragma unroll
+                    for (int i = 0; i < WN; ++i) unpack8(wv[u][i], e.type, f[i]);
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        float g[8];
+                        unpack8(xv[u][r], e.type, g);
+#pragma unroll
+                        for (int i = 0; i < WN; ++i)
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) acc[i][r] = fmaf(f[i][k], g[k], acc[i][r]);
+                    }
+                }
         }
+    } else {
+#pragma unroll 4
+        for (int c = lane; c < n_in; c += 32) {
+            uint16_t wv[WN], xv[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float xv[8];
-            load8(x + (r < rows ? r : rows - 1) * ld_x + c, e.type, n_in - c, VEC, xv);
+            for (int i = 0; i < WN; ++i) wv[i] = wp[i][c];
+#pragma unroll
+            for (int r = 0; r < R; ++r) xv[r] = xp[r][c];
 #pragma unroll
             for (int i = 0; i < WN; ++i)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) acc[i][r] = fmaf(wv[i][k], xv[k], acc[i][r]);
+                for (int r = 0; r < R; ++r) acc[i][r] = fmaf(get16(wv[i], e.type), get16(xv[r], e.type), acc[i][r]);
         }
     }
 #pragma unroll
@@ -214,15 +257,15 @@ __global__ void __launch_bounds__(128) k_linear_few(const uint16_t* __restrict__
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int o = 16; o; o >>= 1) acc[i][r] += __shfl_xor_sync(kFull, acc[i][r], o);
-    // lane r writes row r
+    // lane i R + r writes output i of row r
+    float v[8] = {};
 #pragma unroll
-    for (int i = 0; i < WN; ++i) {
-        float v[8] = {};
+    for (int i = 0; i < WN; ++i)
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if (lane == r) v[0] = acc[i][r];
-        if (lane < rows && lane < R && o0 + i < n_out) emit8(e, lane, o0 + i, 1, v);
-    }
+            if (lane == i * R + r) v[0] = acc[i][r];
+    const int i = lane / R, r = lane % R;
+    if (i < WN && r < rows && o0 + i < n_out) emit8(e, r, o0 + i, 1, v);
 }
 
 // ---------------------------------------------------------------- tensor cores
@@ -617,28 +660,39 @@ __global__ void __launch_bounds__(256) k_pack(const uint16_t* __restrict__ src, 
 // du = dy act'(u) rounded to the operands' type for the products (du: null to
 // skip), and this row block's column sums of the unrounded values (part: null to
 // skip).  A CTA: 256 columns, 8 threads of a warp row by row.
+template <bool VEC>
 __global__ void __launch_bounds__(256) k_du(const uint16_t* __restrict__ dy, int64_t ld_dy, const float* __restrict__ u,
-                                            int64_t ld_u, int64_t rows, int n_out, int type, int act, bool vec_dy,
-                                            bool vec_u, uint16_t* __restrict__ du, int64_t ld_du, float* __restrict__ part) {
+                                            int64_t ld_u, int64_t rows, int n_out, int type, int act,
+                                            uint16_t* __restrict__ du, int64_t ld_du, float* __restrict__ part) {
     __shared__ float sh[8][256 + 8];
     const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
     const int c = blockIdx.x * 256 + tx * 8, n = n_out - c;
     const int64_t r0 = rows * blockIdx.y / gridDim.y, r1 = rows * (blockIdx.y + 1) / gridDim.y;
     float sum[8] = {};
+    constexpr int U = VEC ? 4 : 1;  // rows in flight
     if (n > 0)
-#pragma unroll 4
-        for (int64_t r = r0 + ty; r < r1; r += 8) {
-            float d[8];
-            load8(dy + r * ld_dy + c, type, n, vec_dy, d);
-            if (act != EE_ACT_NONE) {
-                float v[8];
-                load8(u + r * ld_u + c, EE_FP32, n, vec_u, v);
+        for (int64_t r = r0 + ty; r < r1; r += 8 * U) {
+            uint4 raw[U];
+            float v[U][8], d[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d[e] *= act_slope(v[e], act);
+            for (int k = 0; k < U; ++k) {
+                if (r + 8 * k >= r1) continue;
+                if (VEC) raw[k] = __ldg((const uint4*)(dy + (r + 8 * k) * ld_dy + c));
+                if (act != EE_ACT_NONE) load8(u + (r + 8 * k) * ld_u + c, EE_FP32, VEC ? 8 : n, VEC, v[k]);
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += d[e];
-            if (du) store8(du + r * ld_du + c, type, 8, true, d);
+            for (int k = 0; k < U; ++k) {
+                if (r + 8 * k >= r1) continue;
+                if (VEC) unpack8(raw[k], type, d);
+                else load8(dy + (r + 8 * k) * ld_dy + c, type, n, false, d);
+                if (act != EE_ACT_NONE) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d[e] *= act_slope(v[k][e], act);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += d[e];
+                if (du) store8(du + (r + 8 * k) * ld_du + c, type, 8, true, d);
+            }
         }
     if (!part) return;
 #pragma unroll
@@ -648,14 +702,6 @@ __global__ void __launch_bounds__(256) k_du(const uint16_t* __restrict__ dy, int
     for (int i = 0; i < 8; ++i) v += sh[i][threadIdx.x];
     const int col = blockIdx.x * 256 + threadIdx.x;
     if (col < n_out) part[(int64_t)blockIdx.y * n_out + col] = v;
-}
-
-__global__ void __launch_bounds__(256) k_sum_blocks(const float* __restrict__ part, int n, int d, float* __restrict__ out) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= d) return;
-    float v = 0.f;
-    for (int i = 0; i < n; ++i) v += part[(int64_t)i * d + c];
-    out[c] = v;
 }
 
 // ---------------------------------------------------------------- host side
@@ -894,7 +940,7 @@ int forward(const ee_linear_args& a, Ctx& c) {
     e.vec_pre = vec_ok(a.preact, a.n_out, EE_FP32);
     if (a.rows <= kFewRows) {
         if (c.dry) return EE_OK;
-        const bool vec = vec_ok(a.x, a.ld_x, a.type) && vec_ok(a.w, a.ld_w, a.type);
+        const bool vec = a.n_in % 8 == 0 && vec_ok(a.x, a.ld_x, a.type) && vec_ok(a.w, a.ld_w, a.type);
         if (a.rows == 1) return vec ? launch_few<1, true>(a, c, e) : launch_few<1, false>(a, c, e);
         if (a.rows == 2) return vec ? launch_few<2, true>(a, c, e) : launch_few<2, false>(a, c, e);
         if (a.rows <= 4) return vec ? launch_few<4, true>(a, c, e) : launch_few<4, false>(a, c, e);
@@ -944,11 +990,17 @@ int backward(const ee_linear_grad_args& a, Ctx& c) {
         const int blocks = (int)std::max<int64_t>(1, std::min<int64_t>((a.rows + 31) / 32, 4 * c.n_sm / cols));
         float* part = a.dbias ? (float*)c.mem.take(4 * (size_t)blocks * a.n_out) : nullptr;
         if (!c.dry) {
-            k_du<<<dim3(cols, blocks), 256, 0, c.s>>>(du.p, a.ld_dy, a.preact, a.n_out, a.rows, a.n_out, a.type,
-                                                      a.activation, vec_ok(a.dy, a.ld_dy, a.type),
-                                                      vec_ok(a.preact, a.n_out, EE_FP32), p, ld, part);
-            if (part) k_sum_blocks<<<n_blocks(a.n_out, 256), 256, 0, c.s>>>(part, blocks, a.n_out, a.dbias);
-            if ((rc = cuda_status(cudaGetLastError())) != EE_OK) return rc;
+            const bool vec = a.n_out % 8 == 0 && vec_ok(a.dy, a.ld_dy, a.type) && vec_ok(a.preact, a.n_out, EE_FP32);
+            const dim3 grid(cols, blocks);
+            if (vec)
+                k_du<true><<<grid, 256, 0, c.s>>>(du.p, a.ld_dy, a.preact, a.n_out, a.rows, a.n_out, a.type, a.activation, p, ld,
+                                                  part);
+            else
+                k_du<false><<<grid, 256, 0, c.s>>>(du.p, a.ld_dy, a.preact, a.n_out, a.rows, a.n_out, a.type, a.activation, p, ld,
+                                                   part);
+            rc = cuda_status(cudaGetLastError());
+            if (rc == EE_OK && part) rc = cuda_status(launch_sum_parts(part, blocks, a.n_out, a.dbias, c.s));
+            if (rc != EE_OK) return rc;
         }
         if (act && products) {
             du.p = p;

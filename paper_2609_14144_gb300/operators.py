@@ -13,19 +13,19 @@ returned.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 
 import torch
 
 from . import _lib
-from ._lib import check
+from ._lib import EE_ENOMEM, EE_OK, check
 
 __all__ = ["linear", "linear_backward", "rms_norm", "rms_norm_backward", "token_logprobs", "distill_topk",
            "distill_topk_step", "distill_topk_backward"]
 
 _TYPES = {torch.bfloat16: _lib.BF16, torch.float16: _lib.FP16, torch.float32: _lib.FP32}
 _ACTS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu": 3}
+_FP32, _INT32 = torch.float32, torch.int32
 
 
 def _type(t, name: str) -> int:
@@ -35,86 +35,81 @@ def _type(t, name: str) -> int:
         raise ValueError(f"{name} must be bfloat16, float16 or float32, not {t.dtype}") from None
 
 
-def _mat(t, name: str, rows=None, cols=None, dtype=None) -> int:
-    """Checks a matrix and returns its row stride."""
-    if not t.is_cuda:
+def _device(t, name: str) -> int:
+    """Index of the CUDA device of the tensor that a call goes by."""
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
-        raise ValueError(f"{name} must have shape [{'rows' if rows is None else rows}, "
-                         f"{'width' if cols is None else cols}], not {list(t.shape)}")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name} must have unit stride along its rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    return dev
 
 
-def _vec(t, name: str, n: int, dtype=None):
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name} must be contiguous with {n} elements")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+def _elsewhere(dev: int, stream) -> bool:
+    """The call is not for the current device and stream (_placed makes it so)."""
+    return stream is not None or dev != torch.cuda.current_device()
 
 
-def _full(t, name: str, shape, dtype):
-    """Checks a contiguous tensor that the caller passes for a result."""
-    if not t.is_cuda or tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} CUDA tensor of shape {list(shape)}")
+class _placed:
+    """Makes the device and the stream current, so that what a call allocates
+    belongs to the stream that uses it."""
 
-
-@contextlib.contextmanager
-def _other_device_or_stream(device, stream):
-    with torch.cuda.device(device):
-        if stream is None:
-            yield torch.cuda.current_stream(device)
-        else:
-            with torch.cuda.stream(stream):
-                yield stream
-
-
-class _Here:
-    """The common case of _on: the current device and stream."""
-
-    def __init__(self, device):
-        self.stream = torch.cuda.current_stream(device)
+    def __init__(self, dev: int, stream):
+        self.parts = [torch.cuda.device(dev)] + ([] if stream is None else [torch.cuda.stream(stream)])
 
     def __enter__(self):
-        return self.stream
+        for p in self.parts:
+            p.__enter__()
 
     def __exit__(self, *exc):
-        return False
+        for p in reversed(self.parts):
+            p.__exit__(*exc)
 
 
-def _on(ref, stream):
-    """Context in which tensors are allocated and kernels launched: ref's
-    device and the given stream, so that the memory belongs to the stream that
-    uses it."""
-    if stream is None and ref.device.index == torch.cuda.current_device():
-        return _Here(ref.device)
-    return _other_device_or_stream(ref.device, stream)
+# the current stream's handle without the Python object around it
+_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _same_device(ref, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != ref.device:
-            raise ValueError(f"{name} is on {t.device}, not {ref.device}")
+def _mat(t, name: str, dev: int, rows: int, cols: int, dtype=None) -> int:
+    """Checks a matrix (rows or cols below 0: any number) and returns its row stride."""
+    shape = t.shape
+    if len(shape) != 2 or (rows >= 0 and shape[0] != rows) or (cols >= 0 and shape[1] != cols):
+        raise ValueError(f"{name} must have shape [{'rows' if rows < 0 else rows}, {'width' if cols < 0 else cols}], "
+                         f"not {list(shape)}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on CUDA device {dev}, not {t.device}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    ld, unit = t.stride()
+    if unit != 1 and shape[1] > 1:
+        raise ValueError(f"{name} must have unit stride along its rows")
+    return ld if shape[0] > 1 else max(shape[1], ld)
+
+
+def _vec(t, name: str, dev: int, n: int, dtype=None):
+    if len(t.shape) != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be contiguous with {n} elements")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} must be on CUDA device {dev}, not {t.device}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+
+
+def _full(t, name: str, dev: int, shape, dtype):
+    """Checks a contiguous tensor."""
+    if t.get_device() != dev or tuple(t.shape) != shape or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {list(shape)} on CUDA device {dev}")
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
-def _scratch(nbytes: int, given, device):
+def _scratch(nbytes: int, given, ref):
     """Memory for a call's intermediate values: the caller's, if it is enough."""
-    if nbytes == 0:
-        return None
     if given is not None:
-        if given.device != device or not given.is_contiguous() or given.numel() * given.element_size() < nbytes:
-            raise ValueError(f"scratch must be a contiguous tensor of at least {nbytes} bytes on {device}")
+        if given.get_device() != ref.get_device() or not given.is_contiguous() or given.numel() * given.element_size() < nbytes:
+            raise ValueError(f"scratch must be a contiguous tensor of at least {nbytes} bytes on {ref.device}")
         return given
-    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return ref.new_empty(nbytes, dtype=torch.uint8)
 
 
 def _activation(name) -> int:
@@ -122,6 +117,20 @@ def _activation(name) -> int:
         return _ACTS[name]
     except (KeyError, TypeError):
         raise ValueError(f"unknown activation {name!r}") from None
+
+
+def _with_scratch(call, size, args, given, ref, stream: int):
+    """call(args, scratch, bytes, stream); most sizes need no scratch, so it is
+    asked for only when the call without has been refused for it."""
+    a = ctypes.byref(args)
+    rc = call(a, None, 0, stream)
+    if rc == EE_ENOMEM:
+        nb = ctypes.c_size_t(0)
+        check(size(a, ctypes.byref(nb)))
+        mem = _scratch(nb.value, given, ref)
+        rc = call(a, mem.data_ptr(), nb.value, stream)
+    if rc != EE_OK:
+        check(rc)
 
 
 # ---------------------------------------------------------------- affine maps
@@ -132,28 +141,29 @@ def linear(x, w, bias=None, residual=None, activation=None, out_dtype=None, keep
     out_dtype=torch.float32; a residual has the result's.  activation: None,
     "relu", "silu" or "gelu".  keep_preact=True also returns x w^T + bias in fp32,
     which linear_backward needs behind an activation."""
-    lib = _lib.load()
-    ld_x = _mat(x, "x")
+    lib, dev = _lib.load(), _device(x, "x")
+    if _elsewhere(dev, stream):
+        with _placed(dev, stream):
+            return linear(x, w, bias, residual, activation, out_dtype, keep_preact, out, scratch)
+    dtype = x.dtype
+    ld_x = _mat(x, "x", dev, -1, -1)
     rows, n_in = x.shape
-    ld_w = _mat(w, "w", None, n_in, x.dtype)
+    ld_w = _mat(w, "w", dev, -1, n_in, dtype)
     n_out = w.shape[0]
-    out_dtype = out_dtype or (x.dtype if out is None else out.dtype)
+    if out_dtype is None:
+        out_dtype = dtype if out is None else out.dtype
     if bias is not None:
-        _vec(bias, "bias", n_out, x.dtype)
-    ld_r = n_out if residual is None else _mat(residual, "residual", rows, n_out, out_dtype)
+        _vec(bias, "bias", dev, n_out, dtype)
+    ld_r = n_out if residual is None else _mat(residual, "residual", dev, rows, n_out, out_dtype)
     act = _activation(activation)
-    _same_device(x, w=w, bias=bias, residual=residual, out=out)
-    with _on(x, stream) as s:
-        if out is None:
-            out = torch.empty((rows, n_out), dtype=out_dtype, device=x.device)
-        ld_o = _mat(out, "out", rows, n_out, out_dtype)
-        pre = torch.empty((rows, n_out), dtype=torch.float32, device=x.device) if keep_preact else None
-        a = _lib.LinearArgs(_type(x, "x"), _type(out, "out"), act, n_in, n_out, rows, x.data_ptr(), ld_x, w.data_ptr(),
-                            ld_w, _ptr(bias), _ptr(residual), ld_r, out.data_ptr(), ld_o, _ptr(pre))
-        nb = ctypes.c_size_t(0)
-        check(lib.ee_linear_scratch_bytes(ctypes.byref(a), ctypes.byref(nb)))
-        mem = _scratch(nb.value, scratch, x.device)
-        check(lib.ee_linear(ctypes.byref(a), _ptr(mem), nb.value, s.cuda_stream))
+    if out is None:
+        out, ld_o = x.new_empty((rows, n_out), dtype=out_dtype), n_out
+    else:
+        ld_o = _mat(out, "out", dev, rows, n_out, out_dtype)
+    pre = x.new_empty((rows, n_out), dtype=_FP32) if keep_preact else None
+    a = _lib.LinearArgs(_type(x, "x"), _type(out, "out"), act, n_in, n_out, rows, x.data_ptr(), ld_x, w.data_ptr(), ld_w,
+                        _ptr(bias), _ptr(residual), ld_r, out.data_ptr(), ld_o, _ptr(pre))
+    _with_scratch(lib.ee_linear, lib.ee_linear_scratch_bytes, a, scratch, x, _stream(dev))
     return (out, pre) if keep_preact else out
 
 
@@ -166,44 +176,43 @@ def linear_backward(dy, x, w, activation=None, preact=None, dx=True, dw=True, db
     dw_dtype=torch.float32; dbias is fp32.  Behind an activation preact is what
     linear(..., keep_preact=True) returned, and dy act'(preact) is rounded to the
     operands' type for the two products."""
-    lib = _lib.load()
-    ld_dy = _mat(dy, "dy")
+    lib, dev = _lib.load(), _device(dy, "dy")
+    if _elsewhere(dev, stream):
+        with _placed(dev, stream):
+            return linear_backward(dy, x, w, activation, preact, dx, dw, dbias, dw_dtype, scratch)
+    dtype = dy.dtype
+    ld_dy = _mat(dy, "dy", dev, -1, -1)
     rows, n_out = dy.shape
     if w is None and x is None:
         raise ValueError("x or w is needed for the shape")
     n_in = (x if w is None else w).shape[-1]
-    ld_x = n_in if x is None else _mat(x, "x", rows, n_in, dy.dtype)
-    ld_w = n_in if w is None else _mat(w, "w", n_out, n_in, dy.dtype)
-    want_dx, want_dw, want_db = (t is not None and t is not False for t in (dx, dw, dbias))
-    if (want_dx and w is None) or (want_dw and x is None):
+    ld_x = n_in if x is None else _mat(x, "x", dev, rows, n_in, dtype)
+    ld_w = n_in if w is None else _mat(w, "w", dev, n_out, n_in, dtype)
+    dx, dw, dbias = (None if t is False else t for t in (dx, dw, dbias))
+    if (dx is not None and w is None) or (dw is not None and x is None):
         raise ValueError("dx needs w, dw needs x")
     act = _activation(activation)
     if act:
         if preact is None:
             raise ValueError("preact is needed behind an activation")
-        _full(preact, "preact", (rows, n_out), torch.float32)
-    _same_device(dy, x=x, w=w, preact=preact if act else None)
-    with _on(dy, stream) as s:
-        if dx is True:
-            dx = torch.empty((rows, n_in), dtype=dy.dtype, device=dy.device)
-        if dw is True:
-            dw = torch.empty((n_out, n_in), dtype=dw_dtype or dy.dtype, device=dy.device)
-        if dbias is True:
-            dbias = torch.empty(n_out, dtype=torch.float32, device=dy.device)
-        ld_dx = _mat(dx, "dx", rows, n_in, dy.dtype) if want_dx else n_in
-        if want_dw:
-            _full(dw, "dw", (n_out, n_in), dw_dtype or dw.dtype)
-        if want_db:
-            _full(dbias, "dbias", (n_out,), torch.float32)
-        dx, dw, dbias = (t if want else None for t, want in ((dx, want_dx), (dw, want_dw), (dbias, want_db)))
-        _same_device(dy, dx=dx, dw=dw, dbias=dbias)
-        a = _lib.LinearGradArgs(_type(dy, "dy"), act, n_in, n_out, rows, dy.data_ptr(), ld_dy, _ptr(x), ld_x, _ptr(w),
-                                ld_w, _ptr(preact) if act else None, _ptr(dx), ld_dx, _ptr(dw),
-                                _type(dw, "dw") if want_dw else 0, 0, _ptr(dbias))
-        nb = ctypes.c_size_t(0)
-        check(lib.ee_linear_backward_scratch_bytes(ctypes.byref(a), ctypes.byref(nb)))
-        mem = _scratch(nb.value, scratch, dy.device)
-        check(lib.ee_linear_backward(ctypes.byref(a), _ptr(mem), nb.value, s.cuda_stream))
+        _full(preact, "preact", dev, (rows, n_out), _FP32)
+    ld_dx = n_in
+    if dx is True:
+        dx = dy.new_empty((rows, n_in))
+    elif dx is not None:
+        ld_dx = _mat(dx, "dx", dev, rows, n_in, dtype)
+    if dw is True:
+        dw = dy.new_empty((n_out, n_in), dtype=dw_dtype or dtype)
+    elif dw is not None:
+        _full(dw, "dw", dev, (n_out, n_in), dw_dtype or dw.dtype)
+    if dbias is True:
+        dbias = dy.new_empty(n_out, dtype=_FP32)
+    elif dbias is not None:
+        _full(dbias, "dbias", dev, (n_out,), _FP32)
+    a = _lib.LinearGradArgs(_type(dy, "dy"), act, n_in, n_out, rows, dy.data_ptr(), ld_dy, _ptr(x), ld_x, _ptr(w), ld_w,
+                            _ptr(preact) if act else None, _ptr(dx), ld_dx, _ptr(dw), 0 if dw is None else _type(dw, "dw"), 0,
+                            _ptr(dbias))
+    _with_scratch(lib.ee_linear_backward, lib.ee_linear_backward_scratch_bytes, a, scratch, dy, _stream(dev))
     return dx, dw, dbias
 
 
@@ -211,48 +220,58 @@ def linear_backward(dy, x, w, activation=None, preact=None, dx=True, dw=True, db
 def rms_norm(x, gain, eps: float, out_dtype=None, out=None, stream=None):
     """(y, rstd): y = x rstd gain with rstd = 1 / sqrt(mean x^2 + eps) per row
     (fp32, for rms_norm_backward).  y has x's type, or out_dtype."""
-    lib = _lib.load()
-    ld_x = _mat(x, "x")
+    lib, dev = _lib.load(), _device(x, "x")
+    if _elsewhere(dev, stream):
+        with _placed(dev, stream):
+            return rms_norm(x, gain, eps, out_dtype, out)
+    ld_x = _mat(x, "x", dev, -1, -1)
     rows, d = x.shape
-    _vec(gain, "gain", d)
-    out_dtype = out_dtype or (x.dtype if out is None else out.dtype)
-    _same_device(x, gain=gain, out=out)
-    with _on(x, stream) as s:
-        if out is None:
-            out = torch.empty((rows, d), dtype=out_dtype, device=x.device)
-        ld_y = _mat(out, "out", rows, d, out_dtype)
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-        check(lib.ee_rms_norm(x.data_ptr(), _type(x, "x"), rows, d, ld_x, gain.data_ptr(), _type(gain, "gain"),
-                              float(eps), out.data_ptr(), _type(out, "out"), ld_y, rstd.data_ptr(), s.cuda_stream))
+    _vec(gain, "gain", dev, d)
+    if out is None:
+        out, ld_y = x.new_empty((rows, d), dtype=out_dtype or x.dtype), d
+    else:
+        ld_y = _mat(out, "out", dev, rows, d, out_dtype)
+    rstd = x.new_empty(rows, dtype=_FP32)
+    rc = lib.ee_rms_norm(x.data_ptr(), _type(x, "x"), rows, d, ld_x, gain.data_ptr(), _type(gain, "gain"), eps,
+                         out.data_ptr(), _type(out, "out"), ld_y, rstd.data_ptr(), _stream(dev))
+    if rc != EE_OK:
+        check(rc)
     return out, rstd
 
 
 def rms_norm_backward(dy, x, gain, rstd, dx=True, dgain=True, scratch=None, stream=None):
     """(dx, dgain) of rms_norm: dx of x's type, dgain fp32 [d].  Each of them is
     True, False (None is returned) or a tensor to write; dx may be dy."""
-    lib = _lib.load()
-    ld_x = _mat(x, "x")
+    lib, dev = _lib.load(), _device(x, "x")
+    if _elsewhere(dev, stream):
+        with _placed(dev, stream):
+            return rms_norm_backward(dy, x, gain, rstd, dx, dgain, scratch)
+    ld_x = _mat(x, "x", dev, -1, -1)
     rows, d = x.shape
-    ld_dy = _mat(dy, "dy", rows, d)
-    _vec(gain, "gain", d)
-    _vec(rstd, "rstd", rows, torch.float32)
-    _same_device(x, dy=dy, gain=gain, rstd=rstd)
-    with _on(x, stream) as s:
-        if dx is True:
-            dx = torch.empty((rows, d), dtype=x.dtype, device=x.device)
+    ld_dy = _mat(dy, "dy", dev, rows, d)
+    _vec(gain, "gain", dev, d)
+    _vec(rstd, "rstd", dev, rows, _FP32)
+    dx, dgain = (None if t is False else t for t in (dx, dgain))
+    ld_dx = d
+    if dx is True:
+        dx = x.new_empty((rows, d))
+    elif dx is not None:
+        ld_dx = _mat(dx, "dx", dev, rows, d, x.dtype)
+    mem, nbytes = None, 0
+    if dgain is not None:
         if dgain is True:
-            dgain = torch.empty(d, dtype=torch.float32, device=x.device)
-        dx, dgain = (None if t is False else t for t in (dx, dgain))
-        ld_dx = d if dx is None else _mat(dx, "dx", rows, d, x.dtype)
-        mem, nb = None, ctypes.c_size_t(0)
-        if dgain is not None:
-            _full(dgain, "dgain", (d,), torch.float32)
-            check(lib.ee_rms_norm_scratch_bytes(rows, d, ctypes.byref(nb)))
-            mem = _scratch(nb.value, scratch, x.device)
-        _same_device(x, dx=dx, dgain=dgain)
-        check(lib.ee_rms_norm_backward(dy.data_ptr(), _type(dy, "dy"), ld_dy, x.data_ptr(), _type(x, "x"), rows, d, ld_x,
-                                       gain.data_ptr(), _type(gain, "gain"), rstd.data_ptr(), _ptr(dx), ld_dx,
-                                       _ptr(dgain), _ptr(mem), nb.value, s.cuda_stream))
+            dgain = x.new_empty(d, dtype=_FP32)
+        else:
+            _full(dgain, "dgain", dev, (d,), _FP32)
+        nb = ctypes.c_size_t(0)
+        check(lib.ee_rms_norm_scratch_bytes(rows, d, ctypes.byref(nb)))
+        nbytes = nb.value
+        mem = _scratch(nbytes, scratch, x) if nbytes else None
+    rc = lib.ee_rms_norm_backward(dy.data_ptr(), _type(dy, "dy"), ld_dy, x.data_ptr(), _type(x, "x"), rows, d, ld_x,
+                                  gain.data_ptr(), _type(gain, "gain"), rstd.data_ptr(), _ptr(dx), ld_dx, _ptr(dgain),
+                                  _ptr(mem), nbytes, _stream(dev))
+    if rc != EE_OK:
+        check(rc)
     return dx, dgain
 
 
@@ -263,52 +282,56 @@ def token_logprobs(logits, ids=None, k: int = 0, temperature: float = 1.0, strea
     below 0: no token, 0 is returned; None: None is returned), the entropy, log sum
     exp(logits / temperature), and the k best tokens with their log p, best first,
     equal logits by the lower index ([rows, k])."""
-    lib = _lib.load()
-    ld = _mat(logits, "logits")
+    lib, dev = _lib.load(), _device(logits, "logits")
+    if _elsewhere(dev, stream):
+        with _placed(dev, stream):
+            return token_logprobs(logits, ids, k, temperature)
+    ld = _mat(logits, "logits", dev, -1, -1)
     rows, vocab = logits.shape
     if ids is not None:
-        _vec(ids, "ids", rows, torch.int32)
-    _same_device(logits, ids=ids)
-    with _on(logits, stream) as s:
-        # one allocation: logprob, entropy, lse, top_logprob
-        dev, k = logits.device, int(k)
-        f = torch.empty(rows * (3 + max(k, 0)), dtype=torch.float32, device=dev)
-        top_ids = torch.empty((rows, max(k, 0)), dtype=torch.int32, device=dev)
-        ent, lse, lp, top = f[:rows], f[rows:2 * rows], f[2 * rows:3 * rows], f[3 * rows:].view(rows, max(k, 0))
-        if ids is None:
-            lp = None
-        check(lib.ee_token_logprobs(logits.data_ptr(), _type(logits, "logits"), rows, vocab, ld, _ptr(ids), k,
-                                    float(temperature), _ptr(lp), ent.data_ptr(), lse.data_ptr(), top.data_ptr(),
-                                    top_ids.data_ptr(), s.cuda_stream))
-    return lp, ent, lse, top, top_ids
+        _vec(ids, "ids", dev, rows, _INT32)
+    n = k if k > 0 else 0
+    # one allocation for the values: entropy, lse, logprob, top_logprob
+    f = logits.new_empty(rows * (3 + n), dtype=_FP32)
+    top_ids = logits.new_empty((rows, n), dtype=_INT32)
+    p = f.data_ptr()
+    rc = lib.ee_token_logprobs(logits.data_ptr(), _type(logits, "logits"), rows, vocab, ld, _ptr(ids), k, temperature,
+                               None if ids is None else p + 8 * rows, p, p + 4 * rows, p + 12 * rows, top_ids.data_ptr(),
+                               _stream(dev))
+    if rc != EE_OK:
+        check(rc)
+    ent, lse, lp, top = f.split((rows, rows, rows, rows * n))
+    return (None if ids is None else lp), ent, lse, top.view(rows, n), top_ids
 
 
-def _lists(logits, ids, teacher):
-    rows = logits.shape[0]
-    ld_i = _mat(ids, "teacher_ids", rows, None, torch.int32)
-    ld_t = _mat(teacher, "teacher", rows, ids.shape[1], torch.float32)
-    _same_device(logits, teacher_ids=ids, teacher=teacher)
-    return ld_i, ld_t, ids.shape[1]
+def _lists(dev: int, rows: int, ids, teacher):
+    ld_i = _mat(ids, "teacher_ids", dev, rows, -1, _INT32)
+    k = ids.shape[1]
+    return ld_i, _mat(teacher, "teacher", dev, rows, k, _FP32), k
 
 
 def _distill(logits, ids, teacher, temperature, tail, weight, grad, want_stats, stream):
-    lib = _lib.load()
-    ld = _mat(logits, "logits")
+    lib, dev = _lib.load(), _device(logits, "logits")
+    if _elsewhere(dev, stream):
+        with _placed(dev, stream):
+            return _distill(logits, ids, teacher, temperature, tail, weight, grad, want_stats, None)
+    ld = _mat(logits, "logits", dev, -1, -1)
     rows, vocab = logits.shape
-    ld_i, ld_t, k = _lists(logits, ids, teacher)
+    ld_i, ld_t, k = _lists(dev, rows, ids, teacher)
     if weight is not None:
-        _vec(weight, "weight", rows, torch.float32)
-    _same_device(logits, weight=weight)
-    with _on(logits, stream) as s:
-        loss = torch.empty(rows, dtype=torch.float32, device=logits.device)
-        stats = torch.empty((rows, 4), dtype=torch.float32, device=logits.device) if want_stats else None
-        if grad is True:
-            grad = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
-        ld_g = vocab if grad is None else _mat(grad, "grad", rows, vocab, logits.dtype)
-        _same_device(logits, grad=grad)
-        check(lib.ee_distill_topk(logits.data_ptr(), _type(logits, "logits"), rows, vocab, ld, ids.data_ptr(), ld_i,
-                                  teacher.data_ptr(), ld_t, k, float(temperature), int(bool(tail)), loss.data_ptr(),
-                                  _ptr(stats), _ptr(weight), _ptr(grad), ld_g, s.cuda_stream))
+        _vec(weight, "weight", dev, rows, _FP32)
+    loss = logits.new_empty(rows, dtype=_FP32)
+    stats = logits.new_empty((rows, 4), dtype=_FP32) if want_stats else None
+    ld_g = vocab
+    if grad is True:
+        grad = logits.new_empty((rows, vocab))
+    elif grad is not None:
+        ld_g = _mat(grad, "grad", dev, rows, vocab, logits.dtype)
+    rc = lib.ee_distill_topk(logits.data_ptr(), _type(logits, "logits"), rows, vocab, ld, ids.data_ptr(), ld_i,
+                             teacher.data_ptr(), ld_t, k, temperature, 1 if tail else 0, loss.data_ptr(), _ptr(stats),
+                             _ptr(weight), _ptr(grad), ld_g, _stream(dev))
+    if rc != EE_OK:
+        check(rc)
     return loss, stats, grad
 
 
@@ -336,18 +359,22 @@ def distill_topk_backward(dloss, logits, teacher_ids, teacher, stats, temperatur
                           grad=None, stream=None):
     """dloss[row] times the gradient of distill_topk's loss, from the same arguments
     and the stats it returned.  grad may be the logits themselves."""
-    lib = _lib.load()
-    ld = _mat(logits, "logits")
+    lib, dev = _lib.load(), _device(logits, "logits")
+    if _elsewhere(dev, stream):
+        with _placed(dev, stream):
+            return distill_topk_backward(dloss, logits, teacher_ids, teacher, stats, temperature, tail, grad)
+    ld = _mat(logits, "logits", dev, -1, -1)
     rows, vocab = logits.shape
-    ld_i, ld_t, k = _lists(logits, teacher_ids, teacher)
-    _vec(dloss, "dloss", rows, torch.float32)
-    _full(stats, "stats", (rows, 4), torch.float32)
-    _same_device(logits, dloss=dloss, stats=stats, grad=grad)
-    with _on(logits, stream) as s:
-        if grad is None:
-            grad = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
-        ld_g = _mat(grad, "grad", rows, vocab, logits.dtype)
-        check(lib.ee_distill_topk_backward(dloss.data_ptr(), logits.data_ptr(), _type(logits, "logits"), rows, vocab, ld,
-                                           teacher_ids.data_ptr(), ld_i, teacher.data_ptr(), ld_t, k, float(temperature),
-                                           int(bool(tail)), stats.data_ptr(), grad.data_ptr(), ld_g, s.cuda_stream))
+    ld_i, ld_t, k = _lists(dev, rows, teacher_ids, teacher)
+    _vec(dloss, "dloss", dev, rows, _FP32)
+    _full(stats, "stats", dev, (rows, 4), _FP32)
+    if grad is None:
+        grad, ld_g = logits.new_empty((rows, vocab)), vocab
+    else:
+        ld_g = _mat(grad, "grad", dev, rows, vocab, logits.dtype)
+    rc = lib.ee_distill_topk_backward(dloss.data_ptr(), logits.data_ptr(), _type(logits, "logits"), rows, vocab, ld,
+                                      teacher_ids.data_ptr(), ld_i, teacher.data_ptr(), ld_t, k, temperature,
+                                      1 if tail else 0, stats.data_ptr(), grad.data_ptr(), ld_g, _stream(dev))
+    if rc != EE_OK:
+        check(rc)
     return grad
