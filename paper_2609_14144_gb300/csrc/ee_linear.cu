@@ -39,9 +39,33 @@ __device__ __forceinline__ float2 unpack2(uint32_t w, int type) {
 __device__ __forceinline__ float get16(uint16_t h, int type) {
     return type == EE_BF16 ? __uint_as_float((uint32_t)h << 16) : __half2float(__ushort_as_half(h));
 }
-__device__ __forceinline__ uint16_t put16(float f, int type) {
-    return type == EE_BF16 ? __bfloat16_as_ushort(__float2bfloat16_rn(f)) : __half_as_ushort(__float2half_rn(f));
+// 2 N values rounded to 16 bits, two per word.
+template <int N>
+__device__ __forceinline__ void pack_words(const float* x, int type, uint32_t* w) {
+    if (type == EE_BF16) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+            w[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+    }
 }
+__device__ __forceinline__ void pack8(const float (&x)[8], int type, uint32_t (&w)[4]) { pack_words<4>(x, type, w); }
+__device__ __forceinline__ void unpack8(const uint4& v, int type, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = unpack2(w[i], type);
+        x[2 * i] = f.x, x[2 * i + 1] = f.y;
+    }
+}
+
 // Eight elements at p, n of them there (16-byte access where `vec`).
 __device__ __forceinline__ void load8(const void* p, int type, int n, bool vec, float (&x)[8]) {
     if (vec && n >= 8) {
@@ -78,8 +102,7 @@ __device__ __forceinline__ void store8(void* p, int type, int n, bool vec, const
         return;
     }
     uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = put16(x[2 * i], type) | (uint32_t)put16(x[2 * i + 1], type) << 16;
+    pack8(x, type, w);
     if (vec && n >= 8) {
         *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
         return;
@@ -176,15 +199,6 @@ __device__ __forceinline__ void emit8x4(const Epilogue& e, int64_t row0, int64_t
 }
 
 // ---------------------------------------------------------------- few rows
-__device__ __forceinline__ void unpack8(const uint4& v, int type, float (&x)[8]) {
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = unpack2(w[i], type);
-        x[2 * i] = f.x, x[2 * i + 1] = f.y;
-    }
-}
-
 // R rows (rows past `rows` repeat the last one and are not written), WN outputs
 // per warp (likewise).  VEC: a lane takes 8 columns of every 256, n_in being a
 // multiple of 8; all loads of a step go out before its first product (a bounds
@@ -281,9 +295,13 @@ template <int BN, bool PAIR>
 struct GShape {
     static constexpr int CG = PAIR ? 2 : 1;
     static constexpr int b_rows = BN / CG, stage = kABytes + b_rows * kTK * 2;
-    static constexpr int ST = 196608 / stage;  // 4 to 8 stages in 192 KB
-    static constexpr int tmem = 2 * BN;        // two accumulators
-    static constexpr size_t smem = (size_t)ST * stage + kEpiWarps * 4096 + 1024 + 512;
+    // an epilogue warp's two blocks of 4 KB for copies to and from the result, or one
+    // (narrow tiles) to bring its rows into order
+    static constexpr bool blocks = BN >= 128;
+    static constexpr int staging = blocks ? 8192 : 4096;
+    static constexpr int ST = (229376 - kEpiWarps * staging) / stage;  // 3 to 8 stages
+    static constexpr int tmem = 2 * BN;                                // two accumulators
+    static constexpr size_t smem = (size_t)ST * stage + kEpiWarps * staging + 1024 + 512;
 };
 
 // Shared-memory descriptor, 128-byte swizzle.  k contiguous: rows of 128 bytes,
@@ -315,6 +333,18 @@ __device__ __forceinline__ void tma_2d(void* dst, const CUtensorMap* map, int c0
             "l"(map), "r"(c0), "r"(c1), "r"(bar)
             : "memory");
 }
+// A block of the result out of shared memory, or of the residual into it.
+__device__ __forceinline__ void tma_out(const CUtensorMap* map, const void* src, int col, int row, int s) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(map), "r"(u_saddr(src)),
+                 "r"(col), "r"(row), "r"(s)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// All but the last N blocks given out have been read from shared memory.
+template <int N>
+__device__ __forceinline__ void tma_out_read() {
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
 __device__ __forceinline__ void expect_tx(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(u_saddr(bar)), "r"(bytes) : "memory");
 }
@@ -325,7 +355,9 @@ __device__ __forceinline__ uint32_t leader_addr(const void* p) {
     return r;
 }
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    // (what it hands on is tensor memory, ordered by the tcgen05 fence: no release of
+    // other memory at cluster scope, which took 1500 cycles)
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void cluster_barrier() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -360,11 +392,33 @@ __device__ __forceinline__ void commit(uint64_t* bar) {
         u_commit(bar);
 }
 
+// 16 columns of this thread's lane of tensor memory.
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// 32 columns; NaN where nothing was summed.
+__device__ __forceinline__ void sums32(uint32_t taddr, bool ok, float (&v)[32]) {
+    uint32_t a[16], b[16];
+    u_ld16(taddr, a);
+    u_ld16(taddr + 16, b);
+    u_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        v[i] = ok ? __uint_as_float(a[i]) : __int_as_float(0x7fffffff);
+        v[16 + i] = ok ? __uint_as_float(b[i]) : __int_as_float(0x7fffffff);
+    }
+}
+
 struct GemmArgs {
     int M, N, nk;        // nk: stages over the whole k range
     int mt, nt, S;       // tiles, k splits
     int chain;           // stages the tensor core adds up by itself
     bool bf16, vec;
+    bool tma;            // results (or partial sums) leave by TMA
     float* part;         // S > 1: partial sums [S][M][ldp]
     int64_t ldp;
     Epilogue e;
@@ -385,18 +439,20 @@ struct GemmArgs {
 // are written as NaN.
 template <int BN, bool PAIR, bool A_MN, bool B_MN>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-    k_gemm(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb, GemmArgs g) {
+    k_gemm(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
+           const __grid_constant__ CUtensorMap mo, const __grid_constant__ CUtensorMap mr, GemmArgs g) {
     using G = GShape<BN, PAIR>;
     constexpr int CG = G::CG;
     extern __shared__ __align__(1024) uint8_t g_smem_raw[];
     uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(g_smem_raw) + 1023) & ~(uintptr_t)1023);
-    float* stage_out = reinterpret_cast<float*>(sm + G::ST * G::stage);
-    uint64_t* full = reinterpret_cast<uint64_t*>(sm + G::ST * G::stage + kEpiWarps * 4096);
+    uint8_t* stage_out = sm + G::ST * G::stage;
+    uint64_t* full = reinterpret_cast<uint64_t*>(stage_out + kEpiWarps * G::staging);
     uint64_t* empty = full + G::ST;
     uint64_t* acc_full = empty + G::ST;
     uint64_t* acc_empty = acc_full + 2;
     uint64_t* done = acc_empty + 2;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(done + 1);
+    uint64_t* res_full = done + 1;  // two per epilogue warp
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(res_full + 2 * kEpiWarps);
     volatile int* stall = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int w = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
@@ -409,6 +465,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             u_mb_init(&acc_empty[i], kEpiWarps * CG);
         }
         u_mb_init(done, 1);
+        for (int i = 0; i < 2 * kEpiWarps; ++i) u_mb_init(&res_full[i], 1);
         *stall = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -525,64 +582,162 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
         asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         const int q = w & 3, h = (w - 4) >> 2;
         constexpr int HC = BN / 2;  // columns of a warp
-        float* so = stage_out + (w - 4) * 1024;
+        uint8_t* so = stage_out + (w - 4) * G::staging;
+        uint64_t* res_bar = res_full + 2 * (w - 4);
         const uint32_t t0 = tmem + ((uint32_t)(32 * q) << 16) + h * HC;
+        const bool f32 = g.S > 1 || g.e.out_type == EE_FP32, tma = G::blocks && g.tma, res = tma && g.S == 1 && g.e.res;
+        const int cw = f32 ? 32 : 64;  // columns of a block of 128-byte rows
         unsigned u = 0;
+        int res_ph = 0;  // phases of the two barriers
         bool ok = true;
         for (int it = first; it < items; it += stride) {
             const int tile = it % tiles, s = it / tiles;
             const int m0 = (tile % g.mt * CG + rank) * kTM + 32 * q, n0 = tile / g.mt * BN + h * HC;
             const int ks = (int)((int64_t)g.nk * (s + 1) / g.S) - (int)((int64_t)g.nk * s / g.S);
-            float acc[HC];
-#pragma unroll
-            for (int i = 0; i < HC; ++i) acc[i] = 0.f;
-            for (int c0 = 0; c0 < ks; c0 += g.chain, ++u) {
+            // the residual's block c of columns into block c & 1 of the staging
+            auto fetch_res = [&](int c) {
+                if (lane == 0 && m0 < g.M && n0 + c * cw < g.N) {
+                    expect_tx(&res_bar[c & 1], 4096);
+                    tma_2d<false>(so + (c & 1) * 4096, &mr, n0 + c * cw, m0, u_saddr(&res_bar[c & 1]));
+                }
+            };
+            if (res && ok) {
+                if (lane == 0) tma_out_read<0>();
+                fetch_res(0);
+                if (cw < HC) fetch_res(1);
+            }
+            auto chain_full = [&] {
                 if (ok && !u_mb_wait(&acc_full[u & 1], (u >> 1) & 1, stall)) {
                     *stall = kErrStall;
                     ok = false;
                 }
-                ok = __all_sync(kFull, ok);  // the loads below are warp-wide
-                if (!ok) break;
+                ok = __all_sync(kFull, ok);  // what follows is warp-wide
                 u_fence_after();
-#pragma unroll
-                for (int c = 0; c < HC; c += 32) {
-                    uint32_t v0[16], v1[16];
-                    u_ld16(t0 + (u & 1) * BN + c, v0);
-                    u_ld16(t0 + (u & 1) * BN + c + 16, v1);
-                    u_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        acc[c + i] += __uint_as_float(v0[i]);
-                        acc[c + 16 + i] += __uint_as_float(v1[i]);
-                    }
-                }
+            };
+            auto chain_read = [&] {
                 u_fence_before();
                 __syncwarp();
                 if (lane == 0) {
                     if (PAIR) arrive_cluster(leader_addr(&acc_empty[u & 1]));
                     else u_mb_arrive(&acc_empty[u & 1]);
                 }
-            }
-            if (!ok) {
+                ++u;
+            };
+            // The item's sums end up in the accumulator of its last chain, from where
+            // they are written a few columns at a time.
+            if (ks <= g.chain) {
+                chain_full();
+            } else {
+                float acc[HC];
 #pragma unroll
-                for (int i = 0; i < HC; ++i) acc[i] = __int_as_float(0x7fffffff);
+                for (int i = 0; i < HC; ++i) acc[i] = 0.f;
+                for (int c0 = 0; c0 < ks; c0 += g.chain) {
+                    chain_full();
+                    const uint32_t t = t0 + (u & 1) * BN;
+#pragma unroll
+                    for (int c = 0; c < HC; c += 32) {
+                        uint32_t v0[16], v1[16];
+                        u_ld16(t + c, v0);
+                        u_ld16(t + c + 16, v1);
+                        u_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            acc[c + i] += __uint_as_float(v0[i]);
+                            acc[c + 16 + i] += __uint_as_float(v1[i]);
+                        }
+                    }
+                    if (c0 + g.chain < ks) chain_read();
+                }
+#pragma unroll
+                for (int c = 0; c < HC; c += 16) {
+                    uint32_t v[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(acc[c + i]);
+                    tmem_st16(t0 + (u & 1) * BN + c, v);
+                }
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
             }
-            if (m0 >= g.M) continue;
-            // 32 x 32 blocks through shared memory, so that four lanes write 32
+            const uint32_t sums = t0 + (u & 1) * BN;
+            if (tma) {
+                // Each lane puts its row of a block (128 bytes) into the staging, swizzled as
+                // the copy expects it, bias and residual added; one copy writes the block and
+                // drops what lies outside the result.
+#pragma unroll 1
+                for (int c = 0; c * cw < HC && n0 + c * cw < g.N && m0 < g.M; ++c) {
+                    uint8_t* blk = so + (c & 1) * 4096 + lane * 128;
+                    const int col = n0 + c * cw, swz = lane & 7;
+                    if (c >= 2 || !res) {  // the copy out of this block two blocks ago
+                        if (lane == 0) tma_out_read<1>();
+                        __syncwarp();
+                    }
+                    if (res) {
+                        if (c >= 2 && ok) fetch_res(c);
+                        if (ok && !u_mb_wait(&res_bar[c & 1], res_ph >> (c & 1) & 1, stall)) {
+                            *stall = kErrStall;
+                            ok = false;
+                        }
+                        ok = __all_sync(kFull, ok);
+                        res_ph ^= 1 << (c & 1);
+                    }
+                    const bool bias = g.S == 1 && g.e.bias;
+#pragma unroll 1
+                    for (int half = 0; half < (f32 ? 1 : 2); ++half) {
+                        const int col32 = col + 32 * half;
+                        float v[32];
+                        sums32(sums + c * cw + 32 * half, ok, v);
+                        if (bias) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                float x[8];
+                                load8((const uint16_t*)g.e.bias + col32 + 8 * j, g.e.type, g.N - col32 - 8 * j, g.e.vec_bias, x);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) v[8 * j + i] += x[i];
+                            }
+                        }
+                        if (f32) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                float4* p = reinterpret_cast<float4*>(blk + ((j ^ swz) << 4));
+                                float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+                                if (res) r = *p;
+                                *p = make_float4(v[4 * j] + r.x, v[4 * j + 1] + r.y, v[4 * j + 2] + r.z, v[4 * j + 3] + r.w);
+                            }
+                        } else {
+                            uint4* p[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) p[j] = reinterpret_cast<uint4*>(blk + (((4 * half + j) ^ swz) << 4));
+                            if (res) {
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    float x[8];
+                                    unpack8(*p[j], g.e.type, x);
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) v[8 * j + i] += x[i];
+                                }
+                            }
+                            uint32_t o[16];
+                            pack_words<16>(v, g.e.type, o);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) *p[j] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+                        }
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) tma_out(&mo, so + (c & 1) * 4096, col, m0, s);
+                }
+                chain_read();
+                continue;
+            }
+            // Otherwise 32 x 32 blocks through shared memory, so that four lanes write 32
             // neighbouring columns of a row: 16-byte pieces, swizzled by the row.
-            // One body for all blocks: unrolled, its instructions came from memory
-            // for every tile (10000 cycles a tile of 128 x 256).
             float4* s4 = reinterpret_cast<float4*>(so);
 #pragma unroll 1
-            for (int c = 0; c < HC && n0 + c < g.N; c += 32) {
+            for (int c = 0; c < HC && n0 + c < g.N && m0 < g.M; c += 32) {
+                float x[32];
+                sums32(sums + c, ok, x);
 #pragma unroll
-                for (int b = 0; b < HC; b += 32)
-                    if (b == c) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            s4[lane * 8 + (j ^ (lane & 7))] =
-                                make_float4(acc[b + 4 * j], acc[b + 4 * j + 1], acc[b + 4 * j + 2], acc[b + 4 * j + 3]);
-                    }
+                for (int j = 0; j < 8; ++j)
+                    s4[lane * 8 + (j ^ (lane & 7))] = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
                 __syncwarp();
                 const int col = n0 + c + 8 * (lane & 3), ch = 2 * (lane & 3), row = m0 + (lane >> 2);
                 auto piece = [&](int i, float (&v)[8]) {
@@ -610,7 +765,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 }
                 __syncwarp();
             }
+            chain_read();
         }
+        if (tma && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
     u_fence_before();
@@ -796,10 +953,36 @@ Tiling tiling(int64_t M, int64_t N, int nk, int n_sm) {
     return best;
 }
 
+// The result [S][M][N] (S > 1: partial sums), or the residual, in blocks of 32 rows
+// of 128 bytes.
+bool make_out_map(CUtensorMap* map, const void* p, int64_t N, int64_t M, int64_t S, int64_t ld, int type, int dims) {
+    auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(tensor_map_encoder());
+    if (!encode) return false;
+    const cuuint64_t dim[3] = {(cuuint64_t)N, (cuuint64_t)M, (cuuint64_t)S};
+    const cuuint64_t row = (cuuint64_t)ld * bytes_of(type), stride[2] = {row, row * (cuuint64_t)M};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / bytes_of(type)), 32, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUtensorMapDataType t = type == EE_BF16   ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                  : type == EE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                    : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+    return encode(map, t, dims, const_cast<void*>(p), dim, stride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int BN, bool PAIR, bool A_MN, bool B_MN>
-int launch_gemm(const Ctx& c, const Mat& A, const Mat& B, const GemmArgs& g) {
+int launch_gemm(const Ctx& c, const Mat& A, const Mat& B, GemmArgs g) {
     using G = GShape<BN, PAIR>;
-    CUtensorMap ma, mb;
+    CUtensorMap ma, mb, mo{}, mr{};
+    // results leave by TMA where their rows allow it and nothing has to be computed
+    // between the sums and the residual
+    const Epilogue& e2 = g.e;
+    g.tma = G::blocks && (g.S > 1 || (e2.act == EE_ACT_NONE && !e2.preact && e2.vec_out && (!e2.res || e2.vec_res)));
+    if (g.tma) {
+        const bool ok = g.S > 1 ? make_out_map(&mo, g.part, g.ldp, g.M, g.S, g.ldp, EE_FP32, 3)
+                                : make_out_map(&mo, e2.out, g.N, g.M, 1, e2.ld_out, e2.out_type, 3) &&
+                                      (!e2.res || make_out_map(&mr, e2.res, g.N, g.M, 1, e2.ld_res, e2.out_type, 2));
+        if (!ok) return fail(EE_ECUDA, "cuTensorMapEncodeTiled failed");
+    }
     if (!make_map(&ma, A, c.type, A_MN ? kTK : kTM) || !make_map(&mb, B, c.type, B_MN ? kTK : G::b_rows))
         return fail(EE_ECUDA, "cuTensorMapEncodeTiled failed");
     auto* k = k_gemm<BN, PAIR, A_MN, B_MN>;
@@ -831,7 +1014,7 @@ int launch_gemm(const Ctx& c, const Mat& A, const Mat& B, const GemmArgs& g) {
     }
     const int64_t items = (int64_t)g.mt * g.nt * g.S;
     cfg.gridDim = dim3((unsigned)(std::min<int64_t>(items, units) * G::CG));
-    return cuda_status(cudaLaunchKernelEx(&cfg, k, ma, mb, g));
+    return cuda_status(cudaLaunchKernelEx(&cfg, k, ma, mb, mo, mr, g));
 }
 
 // D = A B^T.  A_MN / B_MN: the operand is stored with k as its rows.
