@@ -338,7 +338,7 @@ struct Acc {
     template <int N>
     __device__ __forceinline__ void add(uint4 (&v)[N], float vm, float c) {
         constexpr int E = El<DT>::E;
-        // A new reference only when the largest power would pass 2^20: the first chunk
+        // A new reference only when the largest power would pass 2^8: the first chunk
         // sets it, and most threads keep it (following every new maximum, some lane
         // of a warp did in nearly every chunk).
         if (!(vm <= lim) || far) {
@@ -349,7 +349,7 @@ struct Acc {
                 a = pack2(q.a, 0.f);
                 r = ref_of(m, c);
                 far = wide<DT>(m, c);
-                lim = m + 20.f / c;
+                lim = m + 8.f / c;
             }
             if (far) {
 #pragma unroll 1

@@ -2,10 +2,13 @@
 //   r = 1 / sqrt(mean x^2 + eps),  y = x r g
 //   dx = r (g dy - x r^2 mean(g dy x)),  dg = sum over rows of dy x r
 // Both are bound by reading their inputs and writing their result once.  A CTA
-// takes a few rows at a time, so that their loads are in flight together and one
-// barrier serves all their sums; a thread keeps the same columns in every row, so
-// that its share of the gain's gradient stays in registers until the end.
-// 8192 x 2048 bf16: forward 67 MB, backward 101 MB.
+// takes a few rows at a time, so that one barrier serves all their sums; a thread
+// keeps the same columns in every row, so that its share of the gain's gradient
+// stays in registers until the end.  Where rows lie on 16-byte boundaries and there
+// are many, bulk copies bring the next groups of rows into a ring of shared memory
+// meanwhile (k_*_ring): with loads into registers alone an SM had nothing in flight
+// while it reduced and wrote, and 8192 x 2048 bf16 (67 MB forward, 101 MB backward)
+// took 19.3 and 33 us.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -14,6 +17,7 @@
 #include <algorithm>
 
 #include "ee_internal.h"
+#include "ee_umma.cuh"
 
 namespace ee {
 namespace {
@@ -266,6 +270,161 @@ __global__ void __launch_bounds__(CPT == 1 ? 256 : kNormThreads, CPT == 1 ? 3 : 
             store8<false>(part + (int64_t)blockIdx.x * d, EE_FP32, threadIdx.x + i * blockDim.x, d, dg[i]);
 }
 
+// ---------------------------------------------------------------- ring of rows
+struct RowRing {
+    uint64_t full[8];
+    int stall;
+};
+__device__ __forceinline__ void bulk_row(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(u_saddr(dst)),
+                 "l"(src), "r"(bytes), "r"(u_saddr(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void expect_tx(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(u_saddr(bar)), "r"(bytes) : "memory");
+}
+// Rows r0 .. r0 + RB - 1 of one or two matrices (y.p null: one) into a stage.
+template <int RB>
+__device__ void fill(uint8_t* stage, uint64_t* bar, const Rows& x, const Rows& y, int64_t r0, int64_t rows, int d) {
+    const uint32_t bx = (uint32_t)d * bytes_of(x.type), by = y.p ? (uint32_t)d * bytes_of(y.type) : 0;
+    const int n = (int)(rows - r0 < RB ? rows - r0 : RB);
+    expect_tx(bar, n * (bx + by));
+    for (int b = 0; b < n; ++b) {
+        bulk_row(stage + b * bx, row_of(x, r0 + b), bx, bar);
+        if (by) bulk_row(stage + RB * bx + b * by, row_of(y, r0 + b), by, bar);
+    }
+}
+// The wait for a stage; once one ran out (about 2 s), false at once.
+__device__ __forceinline__ bool ready(RowRing& ring, int st, int ph) {
+    if (u_mb_test(&ring.full[st], ph)) return true;
+    volatile int* stall = &ring.stall;
+    const bool ok = *stall == 0 && u_mb_wait(&ring.full[st], ph, nullptr);
+    if (!ok) *stall = 1;
+    return ok;
+}
+__device__ __forceinline__ Raw stage_raw(const uint8_t* row, const int type, int j, int d) {
+    Raw r{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    if (8 * j < d) {
+        const uint4* p = reinterpret_cast<const uint4*>(row + (size_t)8 * j * bytes_of(type));
+        r.a = p[0];
+        if (type == EE_FP32) r.b = p[1];
+    }
+    return r;
+}
+
+// BACK: the backward pass.  XT, YT: types of x (and dx) and of y or dy, known here
+// because with type tests around every conversion, and IEEE quotients and roots per
+// thread, the kernels were bound by their instructions (18 and 32 us for 8192 x 2048
+// bf16 instead of 14.9 and 22.4).  A stage is read into registers before its group's
+// barrier, so that one thread refills it right behind that.
+template <int CPT, int RB, bool BACK, int XT, int YT>
+__global__ void __launch_bounds__(CPT == 1 ? 256 : kNormThreads, CPT == 1 ? 3 : 1)
+    k_rms_norm_ring(Rows x, Rows dy, Rows gain, Rows out, float* __restrict__ rstd, float* __restrict__ part, int64_t rows,
+                    int d, float eps, int stages, int stage_bytes) {
+    constexpr int OT = BACK ? XT : YT;
+    extern __shared__ __align__(128) uint8_t r_smem[];
+    __shared__ __align__(16) float sh[2][kNormThreads / 32][4];
+    __shared__ RowRing ring;
+    const int64_t step = (int64_t)gridDim.x * RB;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < stages; ++i) u_mb_init(&ring.full[i], 1);
+        ring.stall = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        int64_t r0 = (int64_t)blockIdx.x * RB;
+        for (int i = 0; i < stages && r0 < rows; ++i, r0 += step)
+            fill<RB>(r_smem + (size_t)i * stage_bytes, &ring.full[i], x, dy, r0, rows, d);
+    }
+    float g[CPT][8], dg[CPT][8];
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+        to_float(load_raw<true>(gain.p, gain.type, threadIdx.x + i * blockDim.x, d), gain.type, g[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dg[i][e] = 0.f;
+    }
+    __syncthreads();
+    const int bx = d * (XT == EE_FP32 ? 4 : 2), by = d * (YT == EE_FP32 ? 4 : 2);
+    const float inv_d = 1.f / (float)d;
+    int turn = 0, st = 0, ph = 0;
+    for (int64_t r0 = (int64_t)blockIdx.x * RB; r0 < rows; r0 += step, ++turn) {
+        uint8_t* stage = r_smem + (size_t)st * stage_bytes;
+        const bool ok = ready(ring, st, ph);
+        const int n = (int)(rows - r0 < RB ? rows - r0 : RB);  // (rows past the end hold what the stage held before)
+        Raw rx[RB][CPT], ry[RB][CPT];
+        float s[RB], sum[RB];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            sum[b] = 0.f;
+            s[b] = BACK && b < n ? rstd[r0 + b] : 0.f;
+#pragma unroll
+            for (int i = 0; i < CPT; ++i) {
+                const int j = threadIdx.x + i * blockDim.x;
+                rx[b][i] = stage_raw(stage + b * bx, XT, j, d);
+                if (BACK) ry[b][i] = stage_raw(stage + RB * bx + b * by, YT, j, d);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+            if (b < n)
+#pragma unroll
+                for (int i = 0; i < CPT; ++i) {
+                    float v[8];
+                    to_float(rx[b][i], XT, v);
+                    if (!BACK) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum[b] = fmaf(v[e], v[e], sum[b]);
+                    } else {
+                        float y[8];
+                        to_float(ry[b][i], YT, y);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float t = y[e] * v[e];  // (rstd follows)
+                            dg[i][e] = fmaf(t, s[b], dg[i][e]);
+                            sum[b] = fmaf(t, g[i][e], sum[b]);
+                        }
+                    }
+                }
+        if (!ok) {
+#pragma unroll
+            for (int b = 0; b < RB; ++b) sum[b] = __int_as_float(0x7fffffff);
+            dg[0][0] = sum[0];
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // the stage has been read
+        cta_sums<RB>(sum, sh, turn);
+        if (threadIdx.x == 0 && ok && r0 + stages * step < rows)
+            fill<RB>(stage, &ring.full[st], x, dy, r0 + stages * step, rows, d);
+        if (++st == stages) st = 0, ph ^= 1;
+        if (BACK && !out.p) continue;
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            if (b >= n) break;
+            // forward: r; backward: dx = r g dy - (x r) r^2 mean(g dy x)
+            const float m = sum[b] * inv_d, r = BACK ? s[b] : rsqrtf(m + eps), k = r * (r * m);
+#pragma unroll
+            for (int i = 0; i < CPT; ++i) {
+                float v[8];
+                to_float(rx[b][i], XT, v);
+                if (!BACK) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = v[e] * r * g[i][e];
+                } else {
+                    float y[8];
+                    to_float(ry[b][i], YT, y);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = fmaf(r * g[i][e], y[e], -(v[e] * r) * k);
+                }
+                store8<true>((void*)row_of(out, r0 + b), OT, threadIdx.x + i * blockDim.x, d, v);
+            }
+            if (!BACK && rstd && threadIdx.x == 0) rstd[r0 + b] = r;
+        }
+    }
+    if (BACK && part)
+#pragma unroll
+        for (int i = 0; i < CPT; ++i)
+            store8<true>(part + (int64_t)blockIdx.x * d, EE_FP32, threadIdx.x + i * blockDim.x, d, dg[i]);
+    if (threadIdx.x == 0 && ring.stall)  // copies in flight land before the CTA leaves
+        for (int i = 0; i < stages; ++i) u_mb_wait(&ring.full[(st + i) % stages], ph ^ (st + i >= stages), nullptr);
+}
+
 // out = sum of n rows of d, in their order: 16 columns per CTA, 64 groups of rows.
 __global__ void __launch_bounds__(1024) k_sum_parts(const float* __restrict__ part, int n, int d, float* __restrict__ out) {
     __shared__ float sh[64][17];
@@ -307,11 +466,13 @@ int check_rows(const void* p, int type, int64_t rows, int d, int64_t ld) {
 
 // Threads, chunks per thread (one up to 256 threads, 2048 columns) and CTAs: 768
 // threads per SM, four rows at a time where a thread has one chunk (two in the
-// backward pass, which reads two matrices), fewer with more.
+// backward pass, which reads two matrices), fewer with more.  row_bytes: of a row
+// of all inputs where a ring may hold them (0: not); the ring has 2 to 8 stages in
+// 72 KB, so that three CTAs of 256 threads fit an SM.
 struct Plan {
-    int threads, cpt, rb, grid;
+    int threads, cpt, rb, grid, stages, stage_bytes;
 };
-int plan(int64_t rows, int d, bool backward, Plan* p) {
+int plan(int64_t rows, int d, bool backward, int row_bytes, Plan* p) {
     const int chunks = (d + 7) / 8;
     p->cpt = chunks <= 256 ? 1 : chunks <= 512 ? 2 : 4;
     p->rb = backward ? (p->cpt == 1 ? 2 : 1) : 4 / p->cpt;
@@ -319,10 +480,49 @@ int plan(int64_t rows, int d, bool backward, Plan* p) {
     int dev = 0, n_sm = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
-    const int64_t ctas = (int64_t)n_sm * std::max(1, 768 / p->threads);
+    const int per_sm = std::max(1, 768 / p->threads);
+    const int64_t ctas = (int64_t)n_sm * per_sm;
     if ((rows + p->rb - 1) / p->rb < ctas) p->rb = 1;  // few rows: each its own CTA
     p->grid = (int)std::min<int64_t>((rows + p->rb - 1) / p->rb, ctas);
+    p->stage_bytes = row_bytes * p->rb;
+    p->stages = row_bytes ? std::min(8, 216 * 1024 / per_sm / p->stage_bytes) : 0;
+    // a ring pays from the third group of rows on
+    if (p->stages < 2 || rows < (int64_t)3 * p->rb * p->grid || p->rb != (backward ? (p->cpt == 1 ? 2 : 1) : 4 / p->cpt)) p->stages = 0;
     return cuda_status(e);
+}
+struct RingArgs {
+    Plan p;
+    Rows x, dy, gain, out;
+    float *rstd, *part;
+    int64_t rows;
+    int d;
+    float eps;
+    cudaStream_t s;
+};
+template <int CPT, int RB, bool BACK, int XT, int YT>
+int launch_ring(const RingArgs& a) {
+    auto* k = k_rms_norm_ring<CPT, RB, BACK, XT, YT>;
+    const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, 220 * 1024);
+    if (e != cudaSuccess) return cuda_status(e);
+    k<<<a.p.grid, a.p.threads, (size_t)a.p.stages * a.p.stage_bytes, a.s>>>(a.x, a.dy, a.gain, a.out, a.rstd, a.part, a.rows,
+                                                                              a.d, a.eps, a.p.stages, a.p.stage_bytes);
+    return cuda_status(cudaGetLastError());
+}
+template <bool BACK, int XT, int YT>
+int ring_of(const RingArgs& a) {
+    if (a.p.cpt == 1) return launch_ring<1, BACK ? 2 : 4, BACK, XT, YT>(a);
+    if (a.p.cpt == 2) return launch_ring<2, BACK ? 1 : 2, BACK, XT, YT>(a);
+    return launch_ring<4, 1, BACK, XT, YT>(a);
+}
+// The pairs of types that have a ring: alike, or 32-bit rows normalised to 16 bits.
+bool ring_types(int x, int y) { return x == y || x == EE_FP32; }
+template <bool BACK>
+int launch_ring_types(const RingArgs& a, int xt, int yt) {
+    if (xt == EE_BF16) return ring_of<BACK, EE_BF16, EE_BF16>(a);
+    if (xt == EE_FP16) return ring_of<BACK, EE_FP16, EE_FP16>(a);
+    if (yt == EE_BF16) return ring_of<BACK, EE_FP32, EE_BF16>(a);
+    if (yt == EE_FP16) return ring_of<BACK, EE_FP32, EE_FP16>(a);
+    return ring_of<BACK, EE_FP32, EE_FP32>(a);
 }
 bool vec16(const void* p, int64_t ld, int type, int64_t rows) {
     return (uintptr_t)p % 16 == 0 && (rows == 1 || ld * (int64_t)elem(type) % 16 == 0);
@@ -349,11 +549,12 @@ int ee_rms_norm(const void* x, int x_type, int64_t rows, int d, int64_t ld_x, co
     if (rc != EE_OK) return rc;
     if (!(eps >= 0.f)) return fail(EE_EINVAL, "eps must not be negative");
     if (!rows) return EE_OK;
-    Plan p;
-    if ((rc = plan(rows, d, false, &p)) != EE_OK) return rc;
-    const Rows X{x, ld_x, x_type}, G{gain, 0, gain_type}, Y{y, ld_y, y_type};
+    const Rows X{x, ld_x, x_type}, G{gain, 0, gain_type}, Y{y, ld_y, y_type}, none{nullptr, 0, EE_BF16};
     const bool vec = d % 8 == 0 && vec16(x, ld_x, x_type, rows) && vec16(gain, 0, gain_type, 1) && vec16(y, ld_y, y_type, rows);
+    Plan p;
+    if ((rc = plan(rows, d, false, vec && ring_types(x_type, y_type) ? d * (int)elem(x_type) : 0, &p)) != EE_OK) return rc;
     cudaStream_t s = (cudaStream_t)stream;
+    if (p.stages) return launch_ring_types<false>(RingArgs{p, X, none, G, Y, rstd, nullptr, rows, d, eps, s}, x_type, y_type);
     auto go = [&](auto k) { k<<<p.grid, p.threads, 0, s>>>(X, G, Y, rstd, rows, d, eps); };
     if (p.cpt == 1 && p.rb == 1) vec ? go(k_rms_norm<1, 1, true>) : go(k_rms_norm<1, 1, false>);
     else if (p.cpt == 1) vec ? go(k_rms_norm<1, 4, true>) : go(k_rms_norm<1, 4, false>);
@@ -366,7 +567,7 @@ int ee_rms_norm(const void* x, int x_type, int64_t rows, int d, int64_t ld_x, co
 int ee_rms_norm_scratch_bytes(int64_t rows, int d, size_t* bytes) {
     if (!bytes || rows < 0 || d < 1 || d > EE_MAX_NORM) return fail(EE_EINVAL, "bad argument");
     Plan p;
-    const int rc = plan(rows, d, true, &p);
+    const int rc = plan(rows, d, true, 0, &p);
     if (rc != EE_OK) return rc;
     *bytes = 4 * (size_t)p.grid * d;
     return EE_OK;
@@ -384,16 +585,20 @@ int ee_rms_norm_backward(const void* dy, int dy_type, int64_t ld_dy, const void*
     cudaStream_t s = (cudaStream_t)stream;
     if (!rows) return dgain ? cuda_status(cudaMemsetAsync(dgain, 0, 4 * (size_t)d, s)) : EE_OK;
     if (!rstd) return fail(EE_EINVAL, "NULL argument");
-    Plan p;
-    if ((rc = plan(rows, d, true, &p)) != EE_OK) return rc;
-    if (dgain && (!scratch || scratch_bytes < 4 * (size_t)p.grid * d)) return fail(EE_ENOMEM, "scratch too small");
-    if ((uintptr_t)scratch % 16) return fail(EE_EINVAL, "scratch must be 16-byte aligned");
     const Rows Y{dy, ld_dy, dy_type}, X{x, ld_x, x_type}, G{gain, 0, gain_type}, D{dx, ld_dx, x_type};
     const bool vec = d % 8 == 0 && vec16(x, ld_x, x_type, rows) && vec16(gain, 0, gain_type, 1) &&
                      vec16(dy, ld_dy, dy_type, rows) && (!dx || vec16(dx, ld_dx, x_type, rows));
+    Plan p;
+    if ((rc = plan(rows, d, true, vec && ring_types(x_type, dy_type) ? d * (int)(elem(x_type) + elem(dy_type)) : 0, &p)) != EE_OK)
+        return rc;
+    if (dgain && (!scratch || scratch_bytes < 4 * (size_t)p.grid * d)) return fail(EE_ENOMEM, "scratch too small");
+    if ((uintptr_t)scratch % 16) return fail(EE_EINVAL, "scratch must be 16-byte aligned");
     float* part = dgain ? (float*)scratch : nullptr;
     auto go = [&](auto k) { k<<<p.grid, p.threads, 0, s>>>(Y, X, G, rstd, D, part, rows, d); };
-    if (p.cpt == 1 && p.rb == 1) vec ? go(k_rms_norm_backward<1, 1, true>) : go(k_rms_norm_backward<1, 1, false>);
+    if (p.stages) {
+        rc = launch_ring_types<true>(RingArgs{p, X, Y, G, D, const_cast<float*>(rstd), part, rows, d, 0.f, s}, x_type, dy_type);
+        if (rc != EE_OK) return rc;
+    } else if (p.cpt == 1 && p.rb == 1) vec ? go(k_rms_norm_backward<1, 1, true>) : go(k_rms_norm_backward<1, 1, false>);
     else if (p.cpt == 1) vec ? go(k_rms_norm_backward<1, 2, true>) : go(k_rms_norm_backward<1, 2, false>);
     else if (p.cpt == 2) vec ? go(k_rms_norm_backward<2, 1, true>) : go(k_rms_norm_backward<2, 1, false>);
     else vec ? go(k_rms_norm_backward<4, 1, true>) : go(k_rms_norm_backward<4, 1, false>);

@@ -109,7 +109,7 @@ def _scratch(nbytes: int, given, ref):
         if given.get_device() != ref.get_device() or not given.is_contiguous() or given.numel() * given.element_size() < nbytes:
             raise ValueError(f"scratch must be a contiguous tensor of at least {nbytes} bytes on {ref.device}")
         return given
-    return ref.new_empty(nbytes, dtype=torch.uint8)
+    return torch.empty(nbytes, dtype=torch.uint8, device=ref.device)
 
 
 def _activation(name) -> int:
@@ -157,10 +157,10 @@ def linear(x, w, bias=None, residual=None, activation=None, out_dtype=None, keep
     ld_r = n_out if residual is None else _mat(residual, "residual", dev, rows, n_out, out_dtype)
     act = _activation(activation)
     if out is None:
-        out, ld_o = x.new_empty((rows, n_out), dtype=out_dtype), n_out
+        out, ld_o = torch.empty((rows, n_out), dtype=out_dtype, device=x.device), n_out
     else:
         ld_o = _mat(out, "out", dev, rows, n_out, out_dtype)
-    pre = x.new_empty((rows, n_out), dtype=_FP32) if keep_preact else None
+    pre = torch.empty((rows, n_out), dtype=_FP32, device=x.device) if keep_preact else None
     a = _lib.LinearArgs(_type(x, "x"), _type(out, "out"), act, n_in, n_out, rows, x.data_ptr(), ld_x, w.data_ptr(), ld_w,
                         _ptr(bias), _ptr(residual), ld_r, out.data_ptr(), ld_o, _ptr(pre))
     _with_scratch(lib.ee_linear, lib.ee_linear_scratch_bytes, a, scratch, x, _stream(dev))
@@ -198,15 +198,15 @@ def linear_backward(dy, x, w, activation=None, preact=None, dx=True, dw=True, db
         _full(preact, "preact", dev, (rows, n_out), _FP32)
     ld_dx = n_in
     if dx is True:
-        dx = dy.new_empty((rows, n_in))
+        dx = torch.empty((rows, n_in), dtype=dtype, device=dy.device)
     elif dx is not None:
         ld_dx = _mat(dx, "dx", dev, rows, n_in, dtype)
     if dw is True:
-        dw = dy.new_empty((n_out, n_in), dtype=dw_dtype or dtype)
+        dw = torch.empty((n_out, n_in), dtype=dw_dtype or dtype, device=dy.device)
     elif dw is not None:
         _full(dw, "dw", dev, (n_out, n_in), dw_dtype or dw.dtype)
     if dbias is True:
-        dbias = dy.new_empty(n_out, dtype=_FP32)
+        dbias = torch.empty(n_out, dtype=_FP32, device=dy.device)
     elif dbias is not None:
         _full(dbias, "dbias", dev, (n_out,), _FP32)
     a = _lib.LinearGradArgs(_type(dy, "dy"), act, n_in, n_out, rows, dy.data_ptr(), ld_dy, _ptr(x), ld_x, _ptr(w), ld_w,
@@ -228,10 +228,10 @@ def rms_norm(x, gain, eps: float, out_dtype=None, out=None, stream=None):
     rows, d = x.shape
     _vec(gain, "gain", dev, d)
     if out is None:
-        out, ld_y = x.new_empty((rows, d), dtype=out_dtype or x.dtype), d
+        out, ld_y = torch.empty((rows, d), dtype=out_dtype or x.dtype, device=x.device), d
     else:
         ld_y = _mat(out, "out", dev, rows, d, out_dtype)
-    rstd = x.new_empty(rows, dtype=_FP32)
+    rstd = torch.empty(rows, dtype=_FP32, device=x.device)
     rc = lib.ee_rms_norm(x.data_ptr(), _type(x, "x"), rows, d, ld_x, gain.data_ptr(), _type(gain, "gain"), eps,
                          out.data_ptr(), _type(out, "out"), ld_y, rstd.data_ptr(), _stream(dev))
     if rc != EE_OK:
@@ -254,13 +254,13 @@ def rms_norm_backward(dy, x, gain, rstd, dx=True, dgain=True, scratch=None, stre
     dx, dgain = (None if t is False else t for t in (dx, dgain))
     ld_dx = d
     if dx is True:
-        dx = x.new_empty((rows, d))
+        dx = torch.empty((rows, d), dtype=x.dtype, device=x.device)
     elif dx is not None:
         ld_dx = _mat(dx, "dx", dev, rows, d, x.dtype)
     mem, nbytes = None, 0
     if dgain is not None:
         if dgain is True:
-            dgain = x.new_empty(d, dtype=_FP32)
+            dgain = torch.empty(d, dtype=_FP32, device=x.device)
         else:
             _full(dgain, "dgain", dev, (d,), _FP32)
         nb = ctypes.c_size_t(0)
@@ -291,17 +291,17 @@ def token_logprobs(logits, ids=None, k: int = 0, temperature: float = 1.0, strea
     if ids is not None:
         _vec(ids, "ids", dev, rows, _INT32)
     n = k if k > 0 else 0
-    # one allocation for the values: entropy, lse, logprob, top_logprob
-    f = logits.new_empty(rows * (3 + n), dtype=_FP32)
-    top_ids = logits.new_empty((rows, n), dtype=_INT32)
-    p = f.data_ptr()
+    device = logits.device
+    ent = torch.empty(rows, dtype=_FP32, device=device)
+    lse = torch.empty(rows, dtype=_FP32, device=device)
+    lp = None if ids is None else torch.empty(rows, dtype=_FP32, device=device)
+    top = torch.empty((rows, n), dtype=_FP32, device=device)
+    top_ids = torch.empty((rows, n), dtype=_INT32, device=device)
     rc = lib.ee_token_logprobs(logits.data_ptr(), _type(logits, "logits"), rows, vocab, ld, _ptr(ids), k, temperature,
-                               None if ids is None else p + 8 * rows, p, p + 4 * rows, p + 12 * rows, top_ids.data_ptr(),
-                               _stream(dev))
+                               _ptr(lp), ent.data_ptr(), lse.data_ptr(), top.data_ptr(), top_ids.data_ptr(), _stream(dev))
     if rc != EE_OK:
         check(rc)
-    ent, lse, lp, top = f.split((rows, rows, rows, rows * n))
-    return (None if ids is None else lp), ent, lse, top.view(rows, n), top_ids
+    return lp, ent, lse, top, top_ids
 
 
 def _lists(dev: int, rows: int, ids, teacher):
@@ -320,11 +320,11 @@ def _distill(logits, ids, teacher, temperature, tail, weight, grad, want_stats, 
     ld_i, ld_t, k = _lists(dev, rows, ids, teacher)
     if weight is not None:
         _vec(weight, "weight", dev, rows, _FP32)
-    loss = logits.new_empty(rows, dtype=_FP32)
-    stats = logits.new_empty((rows, 4), dtype=_FP32) if want_stats else None
+    loss = torch.empty(rows, dtype=_FP32, device=logits.device)
+    stats = torch.empty((rows, 4), dtype=_FP32, device=logits.device) if want_stats else None
     ld_g = vocab
     if grad is True:
-        grad = logits.new_empty((rows, vocab))
+        grad = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device)
     elif grad is not None:
         ld_g = _mat(grad, "grad", dev, rows, vocab, logits.dtype)
     rc = lib.ee_distill_topk(logits.data_ptr(), _type(logits, "logits"), rows, vocab, ld, ids.data_ptr(), ld_i,
@@ -369,7 +369,7 @@ def distill_topk_backward(dloss, logits, teacher_ids, teacher, stats, temperatur
     _vec(dloss, "dloss", dev, rows, _FP32)
     _full(stats, "stats", dev, (rows, 4), _FP32)
     if grad is None:
-        grad, ld_g = logits.new_empty((rows, vocab)), vocab
+        grad, ld_g = torch.empty((rows, vocab), dtype=logits.dtype, device=logits.device), vocab
     else:
         ld_g = _mat(grad, "grad", dev, rows, vocab, logits.dtype)
     rc = lib.ee_distill_topk_backward(dloss.data_ptr(), logits.data_ptr(), _type(logits, "logits"), rows, vocab, ld,

@@ -243,6 +243,12 @@ def test_rms_norm(rows, d, tx, ty, tg, pad, shift):
         assert torch.equal(z, y)
 
 
+@pytest.mark.parametrize("rows,d,tx,ty", [(6001, 2048, BF16, BF16), (6002, 2040, FP32, BF16), (3001, 4096, FP16, FP16), (1501, 8192, FP32, FP32),
+                                          (50003, 64, BF16, BF16)])
+def test_rms_norm_many_rows(rows, d, tx, ty):
+    test_rms_norm(rows, d, tx, ty, BF16, 0, 0)
+
+
 def test_rms_norm_against_differences_and_special_rows():
     g, h, eps = gen(8), 1e-5, 1e-5
     x, gain, c = normal(g, 30, 100, FP32), normal(g, 1, 100, FP32)[0], normal(g, 30, 100, FP32)
