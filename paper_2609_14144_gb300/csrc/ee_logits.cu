@@ -406,33 +406,39 @@ struct Acc {
 // number of instructions per element (a budget of about 11 per element of two
 // bytes): a chunk that lies wholly in the slice has one wait, one comparison and
 // no other condition.
-constexpr int kNT = 256;                 // consuming threads
-constexpr int kWarps = kNT / 32;
-constexpr int kThreads = kNT + 64;
 constexpr int kPer = 4;                  // vectors per thread and chunk
-constexpr int kChunk = kNT * kPer;       // vectors per stage: 16 KB
 constexpr int kStages = 3;
-constexpr int kCtas = 3;                 // that fit an SM
-constexpr int kRingBytes = kStages * kChunk * 16;
+// NT consuming threads.  The log probabilities take 256 and three CTAs per SM, so
+// that one selects while two stream (145 us for 2048 rows of 151936 with 64 best;
+// 157 with two CTAs of 384); the distillation's rows in flight have to fit in L2,
+// and it takes 384 and two (486 us for 4096 rows; 508 with 256, 521 with three CTAs).
+template <int NT>
+struct Geo {
+    static constexpr int warps = NT / 32, threads = NT + 64;
+    static constexpr int chunk = NT * kPer;  // vectors per stage: 16 or 24 KB
+    static constexpr int ring = kStages * chunk * 16;
+};
+constexpr int kNT = 256, kCtas = 3;    // log probabilities
+constexpr int kDNT = 384, kDCtas = 2;  // distillation
 
 // Words of a slice's listed bits and of the flags over them.
 __host__ __device__ inline int slice_vecs(int vocab, int E, int cs) { return (vocab / E + 2) / cs + 1; }
 __host__ __device__ inline int slice_words(int vocab, int E, int cs) { return (slice_vecs(vocab, E, cs) * E + 31) / 32 + 1; }
 __host__ __device__ inline int slice_flags(int vocab, int E, int cs) {
-    return (slice_vecs(vocab, E, cs) + kChunk - 1) / kChunk * kWarps;
+    return (slice_vecs(vocab, E, cs) + Geo<kDNT>::chunk - 1) / Geo<kDNT>::chunk * Geo<kDNT>::warps;
 }
 
+template <int NT>
 __device__ __forceinline__ void consumers_sync() {
     __syncwarp();  // (the barrier counts a warp as a whole)
-    asm volatile("bar.sync 1, 256;" ::: "memory");
+    asm volatile("bar.sync 1, %0;" ::"n"(NT) : "memory");
 }
-static_assert(kNT == 256, "consumers_sync");
 
-// m: largest value so far (-inf: none); s: sum of 2^t; a: sum of t 2^t.
+template <int NT>
 struct Link {
     uint64_t full[kStages], empty[kStages], list_full[2], list_empty[2], exchange, joined;
     float4 peer[2][kMaxCluster];
-    float4 warp[2][kWarps];
+    float4 warp[2][Geo<NT>::warps];
     int stall;  // a wait ran out: no further wait, results from here on are NaN
 };
 
@@ -446,8 +452,8 @@ __device__ __forceinline__ bool try_wait_cluster(uint64_t* b, int parity) {
     return ok != 0;
 }
 // Waits for the phase of the given parity, at most about 2 s.
-__device__ __noinline__ bool wait_slow(Link& l, uint64_t* b, int parity) {
-    volatile int* stall = &l.stall;
+__device__ __noinline__ bool wait_slow(int* stalled, uint64_t* b, int parity) {
+    volatile int* stall = stalled;
     const long long t0 = clock64();
     for (unsigned it = 1;; ++it) {
         if (try_wait_cluster(b, parity)) return true;
@@ -456,8 +462,9 @@ __device__ __noinline__ bool wait_slow(Link& l, uint64_t* b, int parity) {
     *stall = 1;
     return false;
 }
-__device__ __forceinline__ bool wait(Link& l, uint64_t* b, int parity) {
-    return try_wait_cluster(b, parity) || wait_slow(l, b, parity);
+template <int NT>
+__device__ __forceinline__ bool wait(Link<NT>& l, uint64_t* b, int parity) {
+    return try_wait_cluster(b, parity) || wait_slow(&l.stall, b, parity);
 }
 __device__ __forceinline__ void expect_tx(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(u_saddr(bar)), "r"(bytes) : "memory");
@@ -474,15 +481,16 @@ __device__ __forceinline__ void arrive_at(uint64_t* bar, int rank) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(p) : "memory");
 }
 
-__device__ void link_init(Link& l, int cs) {
+template <int NT>
+__device__ void link_init(Link<NT>& l, int cs) {
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             u_mb_init(&l.full[i], 1);
-            u_mb_init(&l.empty[i], kWarps);
+            u_mb_init(&l.empty[i], Geo<NT>::warps);
         }
         for (int i = 0; i < 2; ++i) {
             u_mb_init(&l.list_full[i], 1);
-            u_mb_init(&l.list_empty[i], kWarps);
+            u_mb_init(&l.list_empty[i], Geo<NT>::warps);
         }
         u_mb_init(&l.exchange, cs);
         u_mb_init(&l.joined, cs > 1 ? cs - 1 : 1);
@@ -502,8 +510,9 @@ struct Turn {
 };
 
 // A CTA's slice of a row.
-template <int DT>
+template <int DT, int NT>
 struct Slice {
+    static constexpr int kChunk = Geo<NT>::chunk;
     Row<DT> row;
     int v0, v1, f0, f1;  // its vectors; those of the row that lie wholly in it
     __device__ Slice(const void* p, int64_t ld, int64_t r, int vocab, int rank, int cs) : row(p, ld, r, vocab) {
@@ -519,8 +528,9 @@ struct Slice {
 
 // Fills the ring with one pass over the slice (one thread).  `n` counts the
 // stages filled so far.
-template <int DT>
-__device__ bool feed(const Slice<DT>& s, uint4* ring, Link& l, Turn& t, int64_t& n) {
+template <int DT, int NT>
+__device__ bool feed(const Slice<DT, NT>& s, uint4* ring, Link<NT>& l, Turn& t, int64_t& n) {
+    constexpr int kChunk = Geo<NT>::chunk;
     for (int vb = s.v0; vb < s.v1; vb += kChunk, t.step(), ++n) {
         if (n >= kStages && !wait(l, &l.empty[t.st], t.ph ^ 1)) return false;
         const int lo = max(vb, s.f0), hi = min(min(vb + kChunk, s.v1), s.f1);
@@ -532,7 +542,8 @@ __device__ bool feed(const Slice<DT>& s, uint4* ring, Link& l, Turn& t, int64_t&
     return true;
 }
 // Every copy lands before the CTA may leave.
-__device__ void drain(Link& l, Turn t, int64_t n) {
+template <int NT>
+__device__ void drain(Link<NT>& l, Turn t, int64_t n) {
     const long long t0 = clock64();
     for (int i = 0; i < kStages && i < n; ++i) {
         // the stage filled i + 1 steps ago
@@ -546,38 +557,39 @@ __device__ void drain(Link& l, Turn t, int64_t n) {
 // reads have to be done before the stage's next bulk copy may be issued, and
 // without it loads that queued behind a burst of stores were overtaken by the
 // arrival (a row's gradient then held powers of the chunk three further on).
-__device__ __forceinline__ void release(Link& l, const Turn& t) {
+template <int NT>
+__device__ __forceinline__ void release(Link<NT>& l, const Turn& t) {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
     if ((threadIdx.x & 31) == 0) u_mb_arrive(&l.empty[t.st]);
 }
 
 // One pass over the slice: many(cur, vb) takes this thread's vectors of a chunk
-// that lies wholly in the slice, vector vb + thread + u kNT being cur[u];
+// that lies wholly in the slice, vector vb + thread + u NT being cur[u];
 // one(w, v, vb) takes vector v of another chunk (-inf past the slice's end, called
 // by warps with any vector in it); after(n) follows the n-th chunk.  False once a
 // wait ran out.
-template <int DT, class Many, class One, class After>
-__device__ __forceinline__ bool consume(const Slice<DT>& s, const uint4* ring, Link& l, Turn& t, Many many, One one,
+template <int DT, int NT, class Many, class One, class After>
+__device__ __forceinline__ bool consume(const Slice<DT, NT>& s, const uint4* ring, Link<NT>& l, Turn& t, Many many, One one,
                                         After after) {
     bool ok = true;
     int n = 0;
-    for (int vb = s.v0; vb < s.v1; vb += kChunk) {
+    for (int vb = s.v0; vb < s.v1; vb += Geo<NT>::chunk) {
         ok &= wait(l, &l.full[t.st], t.ph);
-        const uint4* st = ring + t.st * kChunk + threadIdx.x;
+        const uint4* st = ring + t.st * Geo<NT>::chunk + threadIdx.x;
         if (s.inner(vb)) {
             uint4 cur[kPer];
 #pragma unroll
-            for (int u = 0; u < kPer; ++u) cur[u] = st[u * kNT];
+            for (int u = 0; u < kPer; ++u) cur[u] = st[u * NT];
             release(l, t);
             many(cur, vb);
         } else {
             const int end = min(s.f1, s.v1), warp = threadIdx.x & ~31;
 #pragma unroll 1
-            for (int u = 0; u < kPer && vb + warp + u * kNT < s.v1; ++u) {
-                const int v = vb + threadIdx.x + u * kNT;
+            for (int u = 0; u < kPer && vb + warp + u * NT < s.v1; ++u) {
+                const int v = vb + threadIdx.x + u * NT;
                 uint4 w[1] = {make_uint4(El<DT>::ninf, El<DT>::ninf, El<DT>::ninf, El<DT>::ninf)};
-                if (v >= s.f0 && v < end) w[0] = st[u * kNT];
+                if (v >= s.f0 && v < end) w[0] = st[u * NT];
                 else if (v < s.v1) w[0] = s.row.load_edge((int64_t)v * El<DT>::E - s.row.mis);
                 one(w, v, vb);
             }
@@ -608,8 +620,8 @@ __device__ __forceinline__ Run join_states(const float4* w, int n, float c) {
 }
 // The row's joined softmax from the threads' and, in a cluster, the CTAs'.
 // turn: the row's number; *top (may be null): becomes the CTA's largest.
-template <int DT>
-__device__ __forceinline__ Run row_reduce(Run r, Link& l, float c, int turn, int rank, int cs, float* top) {
+template <int DT, int NT>
+__device__ __forceinline__ Run row_reduce(Run r, Link<NT>& l, float c, int turn, int rank, int cs, float* top) {
     float m = r.m, t = top ? *top : 0.f;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
@@ -624,10 +636,10 @@ __device__ __forceinline__ Run row_reduce(Run r, Link& l, float c, int turn, int
     }
     const int p = turn & 1;
     if ((threadIdx.x & 31) == 0) l.warp[p][threadIdx.x >> 5] = make_float4(m, r.s, r.a, t);
-    consumers_sync();
-    r = join_states<DT>(l.warp[p], kWarps, c);
+    consumers_sync<NT>();
+    r = join_states<DT>(l.warp[p], Geo<NT>::warps, c);
     if (top)
-        for (int i = 0; i < kWarps; ++i) *top = fmaxf(*top, l.warp[p][i].w);
+        for (int i = 0; i < Geo<NT>::warps; ++i) *top = fmaxf(*top, l.warp[p][i].w);
     if (cs > 1) {
         if (threadIdx.x < cs) {
             cg::cluster_group cl = cg::this_cluster();
@@ -691,7 +703,7 @@ __device__ __forceinline__ int2 block_sum(int a, int b, TopShared& sh, int& turn
         if (a) atomicAdd(&sh.sum[slot].x, a);
         if (b) atomicAdd(&sh.sum[slot].y, b);
     }
-    consumers_sync();
+    consumers_sync<kNT>();
     const int2 r = sh.sum[slot];
     if (threadIdx.x == 0) sh.sum[(turn + 2) % 3] = make_int2(0, 0);
     ++turn;
@@ -727,10 +739,10 @@ __device__ int select_best(int n, int k, TopShared& sh, int& turn) {
     if (n > kEnough) {  // (the keys differ, so that at most kEnough reach the prefix in the end)
         const unsigned long long P = key_prefix(sh.keys, n, want, sh, turn);
         if (threadIdx.x == 0) sh.n_surv = 0;
-        consumers_sync();
+        consumers_sync<kNT>();
         for (int i = threadIdx.x; i < n; i += kNT)
             if (sh.keys[i] >= P) sh.surv[atomicAdd(&sh.n_surv, 1)] = sh.keys[i];
-        consumers_sync();
+        consumers_sync<kNT>();
         n = sh.n_surv;
         from = sh.surv;
     }
@@ -741,7 +753,7 @@ __device__ int select_best(int n, int k, TopShared& sh, int& turn) {
         for (int j = 0; j < n; ++j) above += from[j] > me;
         if (above < want) sh.best[above] = me;
     }
-    consumers_sync();
+    consumers_sync<kNT>();
     return want;
 }
 
@@ -755,7 +767,7 @@ __device__ __noinline__ int recollect(const Row<DT>& row, int v0, int v1, int k,
     int above = 0;  // keys known to lie above the prefix
     for (int shift = 56;; shift -= 8) {
         sh.hist[threadIdx.x] = 0;
-        consumers_sync();
+        consumers_sync<kNT>();
         for (int vb = v0; vb < v1; vb += kNT) {
             const int v = vb + threadIdx.x;
             float x[E];
@@ -773,7 +785,7 @@ __device__ __noinline__ int recollect(const Row<DT>& row, int v0, int v1, int k,
                 }
             }
         }
-        consumers_sync();
+        consumers_sync<kNT>();
         if (threadIdx.x == 0) {
             int got = above, d = 255;
             while (d > 0 && got + (int)sh.hist[d] < k) got += (int)sh.hist[d--];
@@ -782,14 +794,14 @@ __device__ __noinline__ int recollect(const Row<DT>& row, int v0, int v1, int k,
             sh.n_surv = got;
             sh.n = 0;
         }
-        consumers_sync();
+        consumers_sync<kNT>();
         prefix = sh.prefix;
         above = sh.n_surv;
         if (sh.done || shift == 0) {
             prefix <<= shift;
             break;
         }
-        consumers_sync();
+        consumers_sync<kNT>();
     }
     for (int v = v0 + threadIdx.x; v < v1; v += kNT) {
         float x[E];
@@ -800,9 +812,9 @@ __device__ __noinline__ int recollect(const Row<DT>& row, int v0, int v1, int k,
             if (x[e] != -kInf && key_of(x[e], idx) >= prefix) push(x[e], idx, sh);
         }
     }
-    consumers_sync();
+    consumers_sync<kNT>();
     const int n = sh.n;
-    consumers_sync();
+    consumers_sync<kNT>();
     return n;
 }
 
@@ -847,7 +859,7 @@ __device__ unsigned mark_bound(int mark, int top, int k, TopShared& ts, int& tur
 // again, from L2.  Group j of thread t: its vectors of chunks [j per, (j + 1)
 // per).  Returns how many are in ts.best.
 template <int DT>
-__device__ int slice_best(const Slice<DT>& s, int groups, int per, unsigned mark, float top, int k, TopShared& ts, int& turn) {
+__device__ int slice_best(const Slice<DT, kNT>& s, int groups, int per, unsigned mark, float top, int k, TopShared& ts, int& turn) {
     constexpr int E = El<DT>::E;
     const int tid = threadIdx.x;
     const unsigned P = mark_bound((int)mark, (int)(order_of(top) >> 16), k, ts, turn);
@@ -860,7 +872,7 @@ __device__ int slice_best(const Slice<DT>& s, int groups, int per, unsigned mark
                 const int at = atomicAdd(&ts.n_hits, 1);
                 if (at < kMaxHits) ts.list[at] = j * kNT + tid;
             }
-    consumers_sync();
+    consumers_sync<kNT>();
     const int hits = ts.n_hits;
     int n = kCand + 1;
     if (hits <= kMaxHits) {
@@ -877,7 +889,7 @@ __device__ int slice_best(const Slice<DT>& s, int groups, int per, unsigned mark
             for (int e = 0; e < E; ++e)
                 if (!(x[e] < thr)) push(x[e], (int)(v * E - s.row.mis + e), ts);
         }
-        consumers_sync();
+        consumers_sync<kNT>();
         n = ts.n;
     }
     if (n > kCand) n = recollect<DT>(s.row, s.v0, s.v1, k, ts);
@@ -897,11 +909,11 @@ struct LogprobArgs {
 // For the best tokens the pass keeps the maximum of every group of vectors, which
 // the running softmax needs anyway; slice_best does the rest.
 template <int DT, bool TOP>
-__global__ void __launch_bounds__(kThreads, kCtas) k_logprobs(LogprobArgs a, int cs) {
+__global__ void __launch_bounds__(Geo<kNT>::threads, kCtas) k_logprobs(LogprobArgs a, int cs) {
     extern __shared__ __align__(128) uint8_t l_smem[];
     uint4* ring = reinterpret_cast<uint4*>(l_smem);
-    Link& l = *reinterpret_cast<Link*>(l_smem + kRingBytes);
-    TopShared& ts = *reinterpret_cast<TopShared*>(l_smem + kRingBytes + sizeof(Link));
+    auto& l = *reinterpret_cast<Link<kNT>*>(l_smem + Geo<kNT>::ring);
+    TopShared& ts = *reinterpret_cast<TopShared*>(l_smem + Geo<kNT>::ring + sizeof(Link<kNT>));
     const int rank = (int)(blockIdx.x % cs), tid = threadIdx.x, stride = gridDim.x / cs;
     if (TOP && tid < 3) ts.sum[tid] = make_int2(0, 0);
     link_init(l, cs);
@@ -910,14 +922,14 @@ __global__ void __launch_bounds__(kThreads, kCtas) k_logprobs(LogprobArgs a, int
         if (tid == kNT) {
             int64_t n = 0;
             for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride)
-                if (!feed(Slice<DT>(a.logits, a.ld, r, a.vocab, rank, cs), ring, l, at, n)) break;
+                if (!feed(Slice<DT, kNT>(a.logits, a.ld, r, a.vocab, rank, cs), ring, l, at, n)) break;
             drain(l, at, n);
         }
     } else {
         const float inv_t = 1.f / a.temperature, c = 1.4426950408889634f / a.temperature;
         int turn = 0, i = 0;
         for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride, ++i) {
-            const Slice<DT> s(a.logits, a.ld, r, a.vocab, rank, cs);
+            const Slice<DT, kNT> s(a.logits, a.ld, r, a.vocab, rank, cs);
             const int chunks = s.chunks(), per = (chunks + kMaxGroups - 1) / kMaxGroups;
             Acc<DT, true> acc;
             int group = 0;
@@ -967,12 +979,12 @@ __global__ void __launch_bounds__(kThreads, kCtas) k_logprobs(LogprobArgs a, int
                         for (int j = tid; j < nb; j += kNT) o->join[(rank - 1) * kMaxList + j] = ts.best[j];
                         if (tid == 0) o->join_n[rank] = nb;
                         asm volatile("fence.acq_rel.cluster;" ::: "memory");
-                        consumers_sync();
+                        consumers_sync<kNT>();
                         if (tid == 0) arrive_at(&l.joined, 0);
                         continue;
                     }
                     if (tid == 0) ts.done = wait(l, &l.joined, i & 1);
-                    consumers_sync();
+                    consumers_sync<kNT>();
                     if (!ts.done) {
                         for (int j = tid; j < a.k; j += kNT) {
                             a.top_logprob[r * a.k + j] = kNan;
@@ -987,7 +999,7 @@ __global__ void __launch_bounds__(kThreads, kCtas) k_logprobs(LogprobArgs a, int
                         for (int j = tid; j < no; j += kNT) ts.keys[n + j] = ts.join[(o - 1) * kMaxList + j];
                         n += no;
                     }
-                    consumers_sync();
+                    consumers_sync<kNT>();
                     nb = select_best(n, a.k, ts, turn);
                 }
                 float* tl = a.top_logprob + r * a.k;
@@ -1086,6 +1098,34 @@ __device__ __forceinline__ void list_read(const DistillArgs& a, const Row<DT>& r
     if (lane < 4 && a.k + lane < kMaxList) ls.id[a.k + lane] = -2;  // (read in fours)
 }
 
+// Whether no earlier entry names entry i's token; ls.next[i].
+__device__ __forceinline__ bool list_first(int k, int i, ListShared& ls) {
+    const int id = ls.id[i];
+    int before = 0, after = 0;  // other entries of the same token
+    const int4* all = reinterpret_cast<const int4*>(ls.id);
+#pragma unroll 4
+    for (int j = 0; j < k; j += 4) {
+        const int4 o = all[j >> 2];
+        before += (j < i && o.x == id) + (j + 1 < i && o.y == id) + (j + 2 < i && o.z == id) + (j + 3 < i && o.w == id);
+        after += (j > i && o.x == id) + (j + 1 > i && o.y == id) + (j + 2 > i && o.z == id) + (j + 3 > i && o.w == id);
+    }
+    const bool first = id >= 0 && before == 0;
+    ls.next[i] = first ? after : -1;
+    return first;
+}
+// ls.merged: what the gradient needs of the weights, q of each token (one warp).
+template <class Q>
+__device__ __forceinline__ void list_merge(int k, ListShared& ls, Q q) {
+    __syncwarp();
+    for (int i = threadIdx.x & 31; i < k; i += 32) {
+        auto sum = q(i);
+        if (ls.next[i] > 0)
+            for (int j = i + 1; j < k; ++j)
+                if (ls.id[j] == ls.id[i]) sum += q(j);
+        ls.merged[i] = (float)sum;
+    }
+}
+
 // What follows from the list by itself (one warp).  The weights and the loss's
 // part are formed in 64 bits: the loss is a small difference of terms q log q and
 // q log p, and q0 one of 1 and sum q; this warp has the time of a row for it.
@@ -1104,17 +1144,7 @@ __device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls) {
     float s = 0.f;
     int listed = 0;
     for (int i = lane; i < a.k; i += 32) {
-        const int id = ls.id[i];
-        int before = 0, after = 0;  // other entries of the same token
-        const int4* all = reinterpret_cast<const int4*>(ls.id);
-#pragma unroll 4
-        for (int j = 0; j < a.k; j += 4) {
-            const int4 o = all[j >> 2];
-            before += (j < i && o.x == id) + (j + 1 < i && o.y == id) + (j + 2 < i && o.z == id) + (j + 3 < i && o.w == id);
-            after += (j > i && o.x == id) + (j + 1 > i && o.y == id) + (j + 2 > i && o.z == id) + (j + 3 > i && o.w == id);
-        }
-        const bool first = id >= 0 && before == 0;
-        ls.next[i] = first ? after : -1;
+        const bool first = list_first(a.k, i, ls);
         listed += first;
         if (first) s += ex2(exponent<DT>(ls.x[i], m, c));
         const double e = exp((double)ls.t[i] - tm);
@@ -1133,14 +1163,7 @@ __device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls) {
         if (q > 0.0 || q != q) part += q * (((double)ls.t[i] - shift) - ls.x[i] * inv_t);
     }
     part = warp_sum(part);
-    __syncwarp();
-    for (int i = lane; i < a.k; i += 32) {
-        double q = ls.q[i];
-        if (ls.next[i] > 0)
-            for (int j = i + 1; j < a.k; ++j)
-                if (ls.id[j] == ls.id[i]) q += ls.q[j];
-        ls.merged[i] = (float)q;
-    }
+    list_merge(a.k, ls, [&](int i) { return ls.q[i]; });
     if (lane == 0) {
         ls.c = part;
         ls.sum = z * scale;
@@ -1152,6 +1175,25 @@ __device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls) {
         ls.q0 = z != z ? kNan : (float)q0;
     }
     __syncwarp();
+}
+
+// The weights alone, in 32 bits: all that the backward pass needs of the list
+// (one warp, in every CTA of a row; the 64-bit form took 21 of its 207 us).
+__device__ void list_weights(const DistillArgs& a, ListShared& ls) {
+    const int lane = threadIdx.x & 31;
+    float tm = -kInf, z = 0.f;
+    for (int i = lane; i < a.k; i += 32) tm = fmaxf(tm, ls.t[i]);
+    tm = warp_max_nan(tm);
+    if (a.tail || tm == -kInf) tm = 0.f;
+    for (int i = lane; i < a.k; i += 32) {
+        list_first(a.k, i, ls);
+        const float e = expf(ls.t[i] - tm);
+        ls.q[i] = e;
+        z += e;
+    }
+    z = warp_sum(z);
+    const float scale = a.tail || z == 0.f ? 1.f : 1.f / z;
+    list_merge(a.k, ls, [&](int i) { return (float)ls.q[i] * scale; });
 }
 
 // Gradient coefficients (x: mo, y: alpha, z: M, w: Q / S) of a row from its list
@@ -1251,30 +1293,30 @@ struct GradRow {
 // gradient's second read of a row comes from L2: the rows in flight fit there
 // (cluster_size).
 template <int DT, bool GRAD>
-__global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) {
+__global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillArgs a, int cs) {
     constexpr int E = El<DT>::E;
     extern __shared__ __align__(128) uint8_t l_smem[];
     uint4* ring = reinterpret_cast<uint4*>(l_smem);
-    Link& l = *reinterpret_cast<Link*>(l_smem + kRingBytes);
-    ListShared* lists = reinterpret_cast<ListShared*>(l_smem + kRingBytes + sizeof(Link));
+    auto& l = *reinterpret_cast<Link<kDNT>*>(l_smem + Geo<kDNT>::ring);
+    ListShared* lists = reinterpret_cast<ListShared*>(l_smem + Geo<kDNT>::ring + sizeof(Link<kDNT>));
     // which vectors of a warp's in a chunk hold listed elements; a bit per element
     uint32_t* flags = reinterpret_cast<uint32_t*>(lists + 2);
     uint32_t* bits = flags + slice_flags(a.vocab, E, cs);
     const int rank = (int)(blockIdx.x % cs), tid = threadIdx.x, stride = gridDim.x / cs;
     const float c = 1.4426950408889634f / a.temperature;
-    for (int i = tid; i < slice_flags(a.vocab, E, cs) + slice_words(a.vocab, E, cs); i += kThreads) flags[i] = 0;
+    for (int i = tid; i < slice_flags(a.vocab, E, cs) + slice_words(a.vocab, E, cs); i += Geo<kDNT>::threads) flags[i] = 0;
     link_init(l, cs);
-    if (tid >= kNT) {
-        if (tid == kNT) {
+    if (tid >= kDNT) {
+        if (tid == kDNT) {
             Turn at;
             int64_t n = 0;
             for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride) {
-                const Slice<DT> s(a.logits, a.ld, r, a.vocab, rank, cs);
+                const Slice<DT, kDNT> s(a.logits, a.ld, r, a.vocab, rank, cs);
                 if (!feed(s, ring, l, at, n)) break;
                 if (GRAD && !(a.weight && a.weight[r] == 0.f) && !feed(s, ring, l, at, n)) break;
             }
             drain(l, at, n);
-        } else if (tid >= kNT + 32) {
+        } else if (tid >= kDNT + 32) {
             int i = 0;
             for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride, ++i) {
                 bool ok = i < 2 || wait(l, &l.list_empty[i & 1], ((i >> 1) - 1) & 1);
@@ -1282,14 +1324,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) 
                 list_read<DT>(a, Row<DT>(a.logits, a.ld, r, a.vocab), r, lists[i & 1], tid & 31, 32);
                 __syncwarp();
                 list_prepare<DT>(a, c, lists[i & 1]);
-                if (tid == kNT + 32) u_mb_arrive(&l.list_full[i & 1]);
+                if (tid == kDNT + 32) u_mb_arrive(&l.list_full[i & 1]);
             }
         }
     } else {
         Turn at;
         int i = 0;
         for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride, ++i) {
-            const Slice<DT> s(a.logits, a.ld, r, a.vocab, rank, cs);
+            const Slice<DT, kDNT> s(a.logits, a.ld, r, a.vocab, rank, cs);
             const ListShared& ls = lists[i & 1];
             bool ok = wait(l, &l.list_full[i & 1], (i >> 1) & 1);
             int bit = -1, flag = 0;
@@ -1297,12 +1339,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) 
                 const int v = (ls.id[tid] + s.row.mis) / E - s.v0;
                 if (v >= 0 && v < s.v1 - s.v0) {
                     bit = v * E + (ls.id[tid] + s.row.mis) % E;
-                    flag = v / kChunk * kWarps + v % kNT / 32;
+                    flag = v / Geo<kDNT>::chunk * Geo<kDNT>::warps + v % kDNT / 32;
                     atomicOr(&bits[bit >> 5], 1u << (bit & 31));
-                    atomicOr(&flags[flag], 1u << (v % kChunk / kNT));
+                    atomicOr(&flags[flag], 1u << (v % Geo<kDNT>::chunk / kDNT));
                 }
             }
-            consumers_sync();
+            consumers_sync<kDNT>();
             Acc<DT, false> acc;
             // the listed elements of vector v out of the way
             auto mask = [&](uint4& w, int v) {
@@ -1313,11 +1355,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) 
             ok &= consume(
                 s, ring, l, at,
                 [&](uint4(&cur)[kPer], int vb) {
-                    const uint32_t here = flags[(vb - s.v0) / kChunk * kWarps + (tid >> 5)];  // (alike for the warp)
+                    const uint32_t here = flags[(vb - s.v0) / Geo<kDNT>::chunk * Geo<kDNT>::warps + (tid >> 5)];  // (alike for the warp)
                     if (here) {
 #pragma unroll
                         for (int u = 0; u < kPer; ++u)
-                            if (here >> u & 1) mask(cur[u], vb + tid + u * kNT);
+                            if (here >> u & 1) mask(cur[u], vb + tid + u * kDNT);
                     }
                     acc.add(cur, max_of<DT>(cur), c);
                 },
@@ -1340,7 +1382,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) 
                 const float w = a.weight ? a.weight[r] : 1.f, f = w * a.temperature;
                 const GradRow<DT> out(a, s.row, r);
                 if (w == 0.f) {  // rows outside the batch: zeros, whatever they hold
-                    for (int v = s.v0 + tid; v < s.v1; v += kNT) out.put(s.row, v, make_uint4(0, 0, 0, 0));
+                    for (int v = s.v0 + tid; v < s.v1; v += kDNT) out.put(s.row, v, make_uint4(0, 0, 0, 0));
                 } else {
                     const GradOf<DT> grad(coef, c, f);
                     ok &= consume(
@@ -1349,10 +1391,10 @@ __global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) 
                             if (out.aligned) {
                                 uint4* to = reinterpret_cast<uint4*>(out.g + ((int64_t)(vb + tid) * E - s.row.mis));
 #pragma unroll
-                                for (int u = 0; u < kPer; ++u) __stcs(to + u * kNT, grad(cur[u]));
+                                for (int u = 0; u < kPer; ++u) __stcs(to + u * kDNT, grad(cur[u]));
                             } else {
 #pragma unroll
-                                for (int u = 0; u < kPer; ++u) out.put(s.row, vb + tid + u * kNT, grad(cur[u]));
+                                for (int u = 0; u < kPer; ++u) out.put(s.row, vb + tid + u * kDNT, grad(cur[u]));
                             }
                         },
                         [&](uint4(&x)[1], int v, int) {
@@ -1360,12 +1402,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_distill(DistillArgs a, int cs) 
                         },
                         [](int) {});
                     if (!ok)  // NaN in every type
-                        for (int v = s.v0 + tid; v < s.v1; v += kNT) out.put(s.row, v, make_uint4(kFull, kFull, kFull, kFull));
+                        for (int v = s.v0 + tid; v < s.v1; v += kDNT) out.put(s.row, v, make_uint4(kFull, kFull, kFull, kFull));
                 }
-                consumers_sync();
-                if (w != 0.f && ok) out.listed(a, s.row, s.v0, s.v1, c, f, coef, ls, kNT);
+                consumers_sync<kDNT>();
+                if (w != 0.f && ok) out.listed(a, s.row, s.v0, s.v1, c, f, coef, ls, kDNT);
             } else {
-                consumers_sync();
+                consumers_sync<kDNT>();
             }
             __syncwarp();
             if ((tid & 31) == 0) u_mb_arrive(&l.list_empty[i & 1]);
@@ -1397,7 +1439,7 @@ __global__ void __launch_bounds__(kBT) k_distill_backward(DistillArgs a, int chu
     for (int u = 0; u < kLU; ++u) nxt[u] = row.load_if(v0 + threadIdx.x + u * kBT, v1);
     list_read<DT>(a, row, r, ls, threadIdx.x, kBT);
     __syncthreads();  // the listed values are read before the row may be overwritten
-    if (threadIdx.x >= kBT - 32) list_prepare<DT>(a, c, ls);
+    if (threadIdx.x >= kBT - 32) list_weights(a, ls);
     for (int vb = v0; vb < v1; vb += kBT * kLU) {
         uint4 cur[kLU];
 #pragma unroll
@@ -1445,11 +1487,11 @@ int check_logits(const void* p, int type, int64_t rows, int vocab, int64_t ld, f
 // by a cluster, as long as every CTA keeps a stage of vectors.  A pass that reads
 // its rows twice shares them until the rows in flight fit in L2 beside what it
 // writes.
-int cluster_size(int64_t rows, int vocab, int type, int n_sm, int ctas, bool twice) {
+int cluster_size(int64_t rows, int vocab, int type, int n_sm, int ctas, int chunk, bool twice) {
     const int64_t bytes = (int64_t)vocab * (int64_t)elem_bytes(type), vecs = bytes / 16;
     int cs = 1;
     while (cs < kMaxCluster &&
-           ((vecs / (2 * cs) >= kChunk &&
+           ((vecs / (2 * cs) >= chunk &&
              (rows * cs < n_sm || (twice && bytes * std::min<int64_t>(rows, ctas * n_sm / cs) > kL2Rows))) ||
             vocab / cs > kMaxSlice))
         cs *= 2;
@@ -1457,13 +1499,13 @@ int cluster_size(int64_t rows, int vocab, int type, int n_sm, int ctas, bool twi
 }
 
 template <class K, class A>
-int launch_rows(K kern, int64_t rows, int cs, int ctas, size_t smem, cudaStream_t s, const A& args) {
+int launch_rows(K kern, int64_t rows, int cs, int ctas, int threads, size_t smem, cudaStream_t s, const A& args) {
     // (one limit for every size: calls of other threads may set it too)
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
     if (e != cudaSuccess) return cuda_status(e);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(std::min<int64_t>(rows, std::max(1, ctas / cs)) * cs));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
@@ -1477,16 +1519,16 @@ int launch_rows(K kern, int64_t rows, int cs, int ctas, size_t smem, cudaStream_
 
 template <int DT>
 int run_logprobs(const LogprobArgs& a, int cs, int n_sm, cudaStream_t s) {
-    const size_t smem = kRingBytes + sizeof(Link);
-    return a.k ? launch_rows(k_logprobs<DT, true>, a.rows, cs, kCtas * n_sm, smem + (cs > 1 ? sizeof(TopShared) : offsetof(TopShared, join)), s, a)
-               : launch_rows(k_logprobs<DT, false>, a.rows, cs, kCtas * n_sm, smem, s, a);
+    const size_t smem = Geo<kNT>::ring + sizeof(Link<kNT>);
+    return a.k ? launch_rows(k_logprobs<DT, true>, a.rows, cs, kCtas * n_sm, Geo<kNT>::threads, smem + (cs > 1 ? sizeof(TopShared) : offsetof(TopShared, join)), s, a)
+               : launch_rows(k_logprobs<DT, false>, a.rows, cs, kCtas * n_sm, Geo<kNT>::threads, smem, s, a);
 }
 
 template <int DT>
 int run_distill(const DistillArgs& a, int cs, int n_sm, cudaStream_t s) {
-    const size_t smem = kRingBytes + sizeof(Link) + 2 * sizeof(ListShared) + 4 * (size_t)(slice_flags(a.vocab, El<DT>::E, cs) + slice_words(a.vocab, El<DT>::E, cs));
-    return a.grad ? launch_rows(k_distill<DT, true>, a.rows, cs, 2 * n_sm, smem, s, a)
-                  : launch_rows(k_distill<DT, false>, a.rows, cs, 2 * n_sm, smem, s, a);
+    const size_t smem = Geo<kDNT>::ring + sizeof(Link<kDNT>) + 2 * sizeof(ListShared) + 4 * (size_t)(slice_flags(a.vocab, El<DT>::E, cs) + slice_words(a.vocab, El<DT>::E, cs));
+    return a.grad ? launch_rows(k_distill<DT, true>, a.rows, cs, kDCtas * n_sm, Geo<kDNT>::threads, smem, s, a)
+                  : launch_rows(k_distill<DT, false>, a.rows, cs, kDCtas * n_sm, Geo<kDNT>::threads, smem, s, a);
 }
 
 int check_list(const int32_t* ids, int64_t ld_ids, const float* teacher, int64_t ld_teacher, int k, int64_t rows) {
@@ -1520,7 +1562,7 @@ int ee_token_logprobs(const void* logits, int type, int64_t rows, int vocab, int
     int n_sm = 0;
     if ((rc = sm_count(&n_sm)) != EE_OK) return rc;
     const LogprobArgs a{logits, ld, rows, vocab, k, ids, temperature, logprob, entropy, lse, top_logprob, top_id};
-    const int cs = cluster_size(rows, vocab, type, n_sm, kCtas, false);
+    const int cs = cluster_size(rows, vocab, type, n_sm, kCtas, Geo<kNT>::chunk, false);
     cudaStream_t s = (cudaStream_t)stream;
     if (type == EE_BF16) return run_logprobs<EE_BF16>(a, cs, n_sm, s);
     if (type == EE_FP16) return run_logprobs<EE_FP16>(a, cs, n_sm, s);
@@ -1539,7 +1581,7 @@ int ee_distill_topk(const void* logits, int type, int64_t rows, int vocab, int64
     if ((uintptr_t)stats % 16) return fail(EE_EINVAL, "stats must be 16-byte aligned");
     int n_sm = 0;
     if ((rc = sm_count(&n_sm)) != EE_OK) return rc;
-    const int cs = cluster_size(rows, vocab, type, n_sm, 2, grad != nullptr);
+    const int cs = cluster_size(rows, vocab, type, n_sm, kDCtas, Geo<kDNT>::chunk, grad != nullptr);
     const DistillArgs a{logits, ld, rows, vocab, k, tail ? 1 : 0, ids, ld_ids, teacher, ld_teacher, temperature, weight, loss,
                         reinterpret_cast<float4*>(stats), grad, ld_grad};
     cudaStream_t s = (cudaStream_t)stream;
