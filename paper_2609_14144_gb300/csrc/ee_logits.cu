@@ -436,7 +436,7 @@ __device__ __forceinline__ void consumers_sync() {
 
 template <int NT>
 struct Link {
-    uint64_t full[kStages], empty[kStages], list_full[2], list_empty[2], exchange, joined;
+    uint64_t full[kStages], empty[kStages], list_ids[2], list_full[2], list_empty[2], exchange, joined;
     float4 peer[2][kMaxCluster];
     float4 warp[2][Geo<NT>::warps];
     int stall;  // a wait ran out: no further wait, results from here on are NaN
@@ -489,6 +489,7 @@ __device__ void link_init(Link<NT>& l, int cs) {
             u_mb_init(&l.empty[i], Geo<NT>::warps);
         }
         for (int i = 0; i < 2; ++i) {
+            u_mb_init(&l.list_ids[i], 1);
             u_mb_init(&l.list_full[i], 1);
             u_mb_init(&l.list_empty[i], Geo<NT>::warps);
         }
@@ -1130,8 +1131,12 @@ __device__ __forceinline__ void list_merge(int k, ListShared& ls, Q q) {
 // part are formed in 64 bits: the loss is a small difference of terms q log q and
 // q log p, and q0 one of 1 and sum q; this warp has the time of a row for it.
 template <int DT>
-__device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls) {
+__device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls, uint64_t* ids_known) {
     const int lane = threadIdx.x & 31;
+    int listed = 0;
+    for (int i = lane; i < a.k; i += 32) listed += list_first(a.k, i, ls);
+    __syncwarp();
+    if (lane == 0) u_mb_arrive(ids_known);  // the row can be streamed meanwhile
     float tm = -kInf, m = -kInf;
     for (int i = lane; i < a.k; i += 32) {
         tm = fmaxf(tm, ls.t[i]);
@@ -1142,11 +1147,8 @@ __device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls) {
     if (a.tail || tm == -kInf) tm = 0.f;
     double z = 0.0;
     float s = 0.f;
-    int listed = 0;
     for (int i = lane; i < a.k; i += 32) {
-        const bool first = list_first(a.k, i, ls);
-        listed += first;
-        if (first) s += ex2(exponent<DT>(ls.x[i], m, c));
+        if (ls.next[i] >= 0) s += ex2(exponent<DT>(ls.x[i], m, c));
         const double e = exp((double)ls.t[i] - tm);
         ls.q[i] = e;
         z += e;
@@ -1323,7 +1325,7 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
                 if (!__all_sync(kFull, ok)) break;
                 list_read<DT>(a, Row<DT>(a.logits, a.ld, r, a.vocab), r, lists[i & 1], tid & 31, 32);
                 __syncwarp();
-                list_prepare<DT>(a, c, lists[i & 1]);
+                list_prepare<DT>(a, c, lists[i & 1], &l.list_ids[i & 1]);
                 if (tid == kDNT + 32) u_mb_arrive(&l.list_full[i & 1]);
             }
         }
@@ -1333,7 +1335,7 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
         for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride, ++i) {
             const Slice<DT, kDNT> s(a.logits, a.ld, r, a.vocab, rank, cs);
             const ListShared& ls = lists[i & 1];
-            bool ok = wait(l, &l.list_full[i & 1], (i >> 1) & 1);
+            bool ok = wait(l, &l.list_ids[i & 1], (i >> 1) & 1);
             int bit = -1, flag = 0;
             if (ok && tid < a.k && ls.next[tid] >= 0) {
                 const int v = (ls.id[tid] + s.row.mis) / E - s.v0;
@@ -1369,6 +1371,7 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
                 },
                 [](int) {});
             Run run = acc.get();
+            ok &= wait(l, &l.list_full[i & 1], (i >> 1) & 1);
             if (!ok) run.s = kNan;
             run = row_reduce<DT>(run, l, c, i, rank, cs, nullptr);
             if (bit >= 0) bits[bit >> 5] = flags[flag] = 0;  // (all are past the row; the next one's are set after the barrier below)
