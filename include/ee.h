@@ -513,7 +513,7 @@ int ee_rms_norm(const void* x, int x_type, int64_t rows, int d, int64_t ld_x, co
                 void* y, int y_type, int64_t ld_y, float* rstd, void* stream);
 /* dx = r (g dy - x r^2 mean(g dy x)), of x's type, and dgain = sum over rows of
  * dy x r, fp32 [d]; either may be NULL.  dx may be dy (same type and stride).
- * scratch (16-byte aligned) is needed for dgain. */
+ * scratch (16-byte aligned) is needed for dgain (0 bytes for a few rows). */
 int ee_rms_norm_scratch_bytes(int64_t rows, int d, size_t* bytes);
 int ee_rms_norm_backward(const void* dy, int dy_type, int64_t ld_dy, const void* x, int x_type, int64_t rows, int d,
                          int64_t ld_x, const void* gain, int gain_type, const float* rstd, void* dx, int64_t ld_dx,

@@ -33,6 +33,7 @@ namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kFewRows = 8;
+constexpr float kNan = __builtin_nanf("");
 
 // ---------------------------------------------------------------- 16-bit values
 __device__ __forceinline__ float2 unpack2(uint32_t w, int type) {
@@ -290,6 +291,8 @@ constexpr int kTM = 128, kTK = 64;        // tile rows; k per stage: 128 bytes
 constexpr int kEpiWarps = 8;
 constexpr int kGemmThreads = 32 * (4 + kEpiWarps);
 constexpr int kABytes = kTM * kTK * 2;
+constexpr int kJoinLd = 64 + 4;           // floats between rows of a split's sums in shared memory
+constexpr int kMaxSplitCluster = 8;
 
 // PAIR: two CTAs of a cluster share a tile of 256 rows (cta_group::2).  Each
 // stages its own 128 rows of A and half of B's, 32 KB a stage instead of 48 for
@@ -411,8 +414,8 @@ __device__ __forceinline__ void sums32(uint32_t taddr, bool ok, float (&v)[32]) 
     u_wait_ld();
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        v[i] = ok ? __uint_as_float(a[i]) : __int_as_float(0x7fffffff);
-        v[16 + i] = ok ? __uint_as_float(b[i]) : __int_as_float(0x7fffffff);
+        v[i] = ok ? __uint_as_float(a[i]) : kNan;
+        v[16 + i] = ok ? __uint_as_float(b[i]) : kNan;
     }
 }
 
@@ -422,6 +425,7 @@ struct GemmArgs {
     int chain;           // stages the tensor core adds up by itself
     bool bf16, vec;
     bool tma;            // results (or partial sums) leave by TMA
+    bool cluster;        // the splits of a tile are a cluster, which joins them
     float* part;         // S > 1: partial sums [S][M][ldp]
     int64_t ldp;
     Epilogue e;
@@ -438,6 +442,9 @@ struct GemmArgs {
 // with chains of 8 stages, 640 cycles each): results of 32 bits take chains of 8
 // (k = 512), results of 16 bits chains of 32, whose drift of at most 128 * 2^-23
 // is far below their rounding.
+// The splits of a narrow tile may be the CTAs of a cluster (one item each): they
+// leave their sums in shared memory and each joins and writes a share of the rows,
+// without another launch.
 // A wait that runs out (about 2 s) ends the CTA's loops; its remaining items
 // are written as NaN.
 template <int BN, bool PAIR, bool A_MN, bool B_MN>
@@ -491,8 +498,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     u_fence_after();
     const uint32_t tmem = *tmem_slot;
     const int rank = PAIR ? (int)(blockIdx.x & 1) : 0;
-    const int first = blockIdx.x / CG, stride = gridDim.x / CG;
     const int tiles = g.mt * g.nt, items = tiles * g.S;
+    constexpr bool kClusters = BN == 64 && !PAIR;
+    const bool cluster = kClusters && g.cluster;
+    const int first = cluster ? blockIdx.x / g.S + blockIdx.x % g.S * tiles : blockIdx.x / CG;
+    const int stride = cluster ? items : gridDim.x / CG;
+    // the set-up above overlaps the kernel before (programmatic launch)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     if (w < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
@@ -737,6 +750,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 chain_read();
                 continue;
             }
+            if (cluster) {  // this split's sums, row by row, where the ring was
+                float* row = reinterpret_cast<float*>(sm) + (32 * q + lane) * kJoinLd + h * HC;
+#pragma unroll
+                for (int c = 0; c < HC; c += 32) {
+                    float x[32];
+                    sums32(sums + c, ok, x);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        *reinterpret_cast<float4*>(row + c + 4 * j) = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
+                }
+                chain_read();
+                continue;
+            }
             // Otherwise 32 x 32 blocks through shared memory, so that four lanes write 32
             // neighbouring columns of a row: 16-byte pieces, swizzled by the row.
             float4* s4 = reinterpret_cast<float4*>(so);
@@ -782,6 +808,34 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     u_fence_before();
     __syncthreads();
     if (PAIR) cluster_barrier();  // the first CTA's MMAs read the second's operands
+    if constexpr (kClusters) {
+        if (cluster) {
+            cluster_barrier();  // every split's sums are there
+            if (w >= 4) {
+                const cg::cluster_group cl = cg::this_cluster();
+                const int tile = blockIdx.x / g.S, s = blockIdx.x % g.S;
+                const int m0 = tile % g.mt * kTM, n0 = tile / g.mt * BN;
+                const int r0 = kTM * s / g.S, r1 = kTM * (s + 1) / g.S;
+                for (int i = threadIdx.x - 128; i < (r1 - r0) * (BN / 8); i += 32 * kEpiWarps) {
+                    const int lr = r0 + i / (BN / 8), lc = i % (BN / 8) * 8, row = m0 + lr, col = n0 + lc;
+                    if (row >= g.M || col >= g.N) continue;
+                    float* at = reinterpret_cast<float*>(sm) + lr * kJoinLd + lc;
+                    float v[8] = {};
+                    for (int k = 0; k < g.S; ++k) {  // in split order
+                        const float4* p = reinterpret_cast<const float4*>(cl.map_shared_rank(at, k));
+                        const float4 a = p[0], b = p[1];
+                        v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
+                        v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
+                        // (a copy that outlasted its wait may have landed on a stalled split's NaN)
+                        if (*cl.map_shared_rank(const_cast<int*>(stall), k)) v[0] = v[1] = v[2] = v[3] = v[4] = v[5] = v[6] = v[7] = kNan;
+                    }
+                    emit8(g.e, row, col, g.N - col, v);
+                }
+            }
+            __syncwarp();
+            cluster_barrier();  // the others have read this CTA's
+        }
+    }
     if (w == 2) {
         if constexpr (PAIR)
             asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(G::tmem) : "memory");
@@ -793,6 +847,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 // The splits' partial sums in split order, then the epilogue; 8 columns per
 // thread.
 __global__ void __launch_bounds__(256) k_join(GemmArgs g) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int64_t chunks = g.ldp / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= chunks * g.M) return;
     const int64_t row = i / chunks;
@@ -995,13 +1051,13 @@ bool make_map(CUtensorMap* map, const Mat& m, int type, int box_rows) {
 // with BN = 256, 900 for the 48 KB of a CTA by itself); set-up and the first copy
 // take 4200, the last tile's write 12 per column; splits write and read their
 // partial sums (about 2400 bytes a cycle over the whole GPU) and take another
-// launch (4000).
+// launch (4000), or join in a cluster (2500; one wave of narrow tiles).
 struct Tiling {
     int bn, S;
-    bool pair;
+    bool pair, cluster;
 };
 Tiling tiling(int64_t M, int64_t N, int nk, int n_sm) {
-    Tiling best{64, 1, false};
+    Tiling best{64, 1, false, false};
     double best_t = 1e30;
     for (int pair = 0; pair < 2; ++pair)
         for (int bn = pair ? 128 : 64; bn <= 256; bn *= 2)
@@ -1011,8 +1067,10 @@ Tiling tiling(int64_t M, int64_t N, int nk, int n_sm) {
                 const double waves = (double)((items + units - 1) / units);
                 const double stage = std::max(2.0 * bn, (kTM + (bn >> pair)) * 128 / 51.0);
                 double t = 4200 + waves * ((nk + S - 1) / S) * stage + 12.0 * bn;
-                if (S > 1) t += 4000 + 8.0 * (double)S * M * N / 2400;
-                if (t < best_t) best_t = t, best = {bn, S, pair != 0};
+                const bool cluster = S > 1 && S <= kMaxSplitCluster && bn == 64 && !pair && items <= n_sm;
+                if (cluster) t += 2500;
+                else if (S > 1) t += 4000 + 8.0 * (double)S * M * N / 2400;
+                if (t < best_t) best_t = t, best = {bn, S, pair != 0, cluster};
             }
     return best;
 }
@@ -1056,12 +1114,14 @@ int launch_gemm(const Ctx& c, const Mat& A, const Mat& B, GemmArgs g) {
     cfg.blockDim = dim3(kGemmThreads);
     cfg.dynamicSmemBytes = G::smem;
     cfg.stream = c.s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = G::CG;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = PAIR ? 2u : (unsigned)g.S;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = PAIR ? 1 : 0;
+    cfg.numAttrs = PAIR || g.cluster ? 2 : 1;
     int units = c.n_sm;
     if (PAIR) {
         // pairs that run at the same time: a cluster lies within a group of SMs, so
@@ -1077,7 +1137,7 @@ int launch_gemm(const Ctx& c, const Mat& A, const Mat& B, GemmArgs g) {
         }
     }
     const int64_t items = (int64_t)g.mt * g.nt * g.S;
-    cfg.gridDim = dim3((unsigned)(std::min<int64_t>(items, units) * G::CG));
+    cfg.gridDim = dim3((unsigned)(g.cluster ? items : std::min<int64_t>(items, units) * G::CG));
     return cuda_status(cudaLaunchKernelEx(&cfg, k, ma, mb, mo, mr, g));
 }
 
@@ -1103,7 +1163,8 @@ int gemm(Ctx& c, Mat A, Mat B, const Epilogue& e) {
     g.S = t.S;
     if ((int64_t)g.mt * g.nt * g.S > 0x7fffffff) return fail(EE_EINVAL, "too many rows");
     g.ldp = (N + 7) / 8 * 8;
-    if (t.S > 1) g.part = (float*)c.mem.take(4 * (size_t)t.S * M * g.ldp);
+    g.cluster = t.cluster;
+    if (t.S > 1 && !t.cluster) g.part = (float*)c.mem.take(4 * (size_t)t.S * M * g.ldp);
     g.e = e;
     if (c.dry) return EE_OK;
     if (t.pair)
@@ -1112,9 +1173,17 @@ int gemm(Ctx& c, Mat A, Mat B, const Epilogue& e) {
         rc = t.bn == 256   ? launch_gemm<256, false, A_MN, B_MN>(c, A, B, g)
              : t.bn == 128 ? launch_gemm<128, false, A_MN, B_MN>(c, A, B, g)
                            : launch_gemm<64, false, A_MN, B_MN>(c, A, B, g);
-    if (rc != EE_OK || t.S == 1) return rc;
-    k_join<<<n_blocks(M * (g.ldp / 8), 256), 256, 0, c.s>>>(g);
-    return cuda_status(cudaGetLastError());
+    if (rc != EE_OK || t.S == 1 || t.cluster) return rc;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(n_blocks(M * (g.ldp / 8), 256));
+    cfg.blockDim = dim3(256);
+    cfg.stream = c.s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cuda_status(cudaLaunchKernelEx(&cfg, k_join, g));
 }
 
 template <int R, bool VEC>

@@ -9,6 +9,7 @@
 // meanwhile (k_*_ring): with loads into registers alone an SM had nothing in flight
 // while it reduced and wrote, and 8192 x 2048 bf16 (67 MB forward, 101 MB backward)
 // took 19.3 and 33 us.
+#include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -18,6 +19,8 @@
 
 #include "ee_internal.h"
 #include "ee_umma.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace ee {
 namespace {
@@ -425,6 +428,78 @@ __global__ void __launch_bounds__(CPT == 1 ? 256 : kNormThreads, CPT == 1 ? 3 : 
         for (int i = 0; i < stages; ++i) u_mb_wait(&ring.full[(st + i) % stages], ph ^ (st + i >= stages), nullptr);
 }
 
+// The backward pass of a few rows in one launch: a cluster of CTAs takes the rows in
+// turn, leaves its shares of the gain's gradient in shared memory and joins them,
+// each CTA a part of the columns.  (Scratch and a second launch for the join took
+// 6 of the 41 us that a forward and a backward pass of 5 rows took with their calls.)
+template <int CPT, bool VEC>
+__global__ void __launch_bounds__(kNormThreads, 1)
+    k_rms_norm_backward_few(Rows dy, Rows x, Rows gain, const float* __restrict__ rstd, Rows dx, float* __restrict__ dgain,
+                            int rows, int d) {
+    extern __shared__ __align__(16) float few_dg[];
+    __shared__ __align__(16) float sh[2][kNormThreads / 32][4];
+    const int cs = (int)gridDim.x;
+    float g[CPT][8], dg[CPT][8];
+#pragma unroll
+    for (int i = 0; i < CPT; ++i) {
+        to_float(load_raw<VEC>(gain.p, gain.type, threadIdx.x + i * blockDim.x, d), gain.type, g[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dg[i][e] = 0.f;
+    }
+    int turn = 0;
+    for (int r = blockIdx.x; r < rows; r += cs, ++turn) {
+        Raw rx[CPT], ry[CPT];
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) {
+            rx[i] = load_raw<VEC>(row_of(x, r), x.type, threadIdx.x + i * blockDim.x, d);
+            ry[i] = load_raw<VEC>(row_of(dy, r), dy.type, threadIdx.x + i * blockDim.x, d);
+        }
+        const float s = rstd[r];
+        float dot[1] = {0.f};
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) {
+            float v[8], y[8];
+            to_float(rx[i], x.type, v);
+            to_float(ry[i], dy.type, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float xh = v[e] * s;
+                dg[i][e] = fmaf(y[e], xh, dg[i][e]);
+                dot[0] = fmaf(y[e] * g[i][e], xh, dot[0]);
+            }
+        }
+        if (!dx.p) continue;
+        cta_sums<1>(dot, sh, turn);
+        const float m = dot[0] / (float)d;
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) {
+            float v[8], y[8];
+            to_float(rx[i], x.type, v);
+            to_float(ry[i], dy.type, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = s * (y[e] * g[i][e] - v[e] * s * m);
+            store8<VEC>((void*)row_of(dx, r), dx.type, threadIdx.x + i * blockDim.x, d, v);
+        }
+    }
+    if (!dgain) return;
+#pragma unroll
+    for (int i = 0; i < CPT; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int c = 8 * (threadIdx.x + i * blockDim.x) + e;
+            if (c < d) few_dg[c] = dg[i][e];
+        }
+    cg::cluster_group cl = cg::this_cluster();
+    cl.sync();
+    const int c1 = d * (blockIdx.x + 1) / cs;
+    for (int c = d * blockIdx.x / cs + threadIdx.x; c < c1; c += blockDim.x) {
+        float v = 0.f;
+        for (int i = 0; i < cs; ++i) v += *cl.map_shared_rank(&few_dg[c], i);
+        dgain[c] = v;
+    }
+    cl.sync();
+}
+
 // out = sum of n rows of d, in their order: 16 columns per CTA, 64 groups of rows.
 __global__ void __launch_bounds__(1024) k_sum_parts(const float* __restrict__ part, int n, int d, float* __restrict__ out) {
     __shared__ float sh[64][17];
@@ -524,6 +599,25 @@ int launch_ring_types(const RingArgs& a, int xt, int yt) {
     if (yt == EE_FP16) return ring_of<BACK, EE_FP32, EE_FP16>(a);
     return ring_of<BACK, EE_FP32, EE_FP32>(a);
 }
+// Rows that one cluster takes in a few turns, their gradient's shares (4 d bytes) in
+// its shared memory.
+bool few_rows(int64_t rows, int d) { return rows <= 32 && d <= 8192; }
+template <class K>
+int launch_few(K k, const Plan& p, const Rows& dy, const Rows& x, const Rows& gain, const float* rstd, const Rows& dx,
+               float* dgain, int rows, int d, cudaStream_t s) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)std::min(rows, 8));
+    cfg.blockDim = dim3((unsigned)p.threads);
+    cfg.dynamicSmemBytes = 4 * (size_t)d;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = cfg.gridDim.x;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cuda_status(cudaLaunchKernelEx(&cfg, k, dy, x, gain, rstd, dx, dgain, rows, d));
+}
 bool vec16(const void* p, int64_t ld, int type, int64_t rows) {
     return (uintptr_t)p % 16 == 0 && (rows == 1 || ld * (int64_t)elem(type) % 16 == 0);
 }
@@ -569,7 +663,7 @@ int ee_rms_norm_scratch_bytes(int64_t rows, int d, size_t* bytes) {
     Plan p;
     const int rc = plan(rows, d, true, 0, &p);
     if (rc != EE_OK) return rc;
-    *bytes = 4 * (size_t)p.grid * d;
+    *bytes = few_rows(rows, d) ? 0 : 4 * (size_t)p.grid * d;
     return EE_OK;
 }
 
@@ -591,8 +685,15 @@ int ee_rms_norm_backward(const void* dy, int dy_type, int64_t ld_dy, const void*
     Plan p;
     if ((rc = plan(rows, d, true, vec && ring_types(x_type, dy_type) ? d * (int)(elem(x_type) + elem(dy_type)) : 0, &p)) != EE_OK)
         return rc;
-    if (dgain && (!scratch || scratch_bytes < 4 * (size_t)p.grid * d)) return fail(EE_ENOMEM, "scratch too small");
+    const bool few = few_rows(rows, d);
+    if (dgain && !few && (!scratch || scratch_bytes < 4 * (size_t)p.grid * d)) return fail(EE_ENOMEM, "scratch too small");
     if ((uintptr_t)scratch % 16) return fail(EE_EINVAL, "scratch must be 16-byte aligned");
+    if (few) {
+        auto one = [&](auto k) { return launch_few(k, p, Y, X, G, rstd, D, dgain, (int)rows, d, s); };
+        if (p.cpt == 1) return vec ? one(k_rms_norm_backward_few<1, true>) : one(k_rms_norm_backward_few<1, false>);
+        if (p.cpt == 2) return vec ? one(k_rms_norm_backward_few<2, true>) : one(k_rms_norm_backward_few<2, false>);
+        return vec ? one(k_rms_norm_backward_few<4, true>) : one(k_rms_norm_backward_few<4, false>);
+    }
     float* part = dgain ? (float*)scratch : nullptr;
     auto go = [&](auto k) { k<<<p.grid, p.threads, 0, s>>>(Y, X, G, rstd, D, part, rows, d); };
     if (p.stages) {

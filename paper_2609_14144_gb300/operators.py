@@ -257,19 +257,21 @@ def rms_norm_backward(dy, x, gain, rstd, dx=True, dgain=True, scratch=None, stre
         dx = torch.empty((rows, d), dtype=x.dtype, device=x.device)
     elif dx is not None:
         ld_dx = _mat(dx, "dx", dev, rows, d, x.dtype)
-    mem, nbytes = None, 0
-    if dgain is not None:
-        if dgain is True:
-            dgain = torch.empty(d, dtype=_FP32, device=x.device)
-        else:
-            _full(dgain, "dgain", dev, (d,), _FP32)
+    if dgain is True:
+        dgain = torch.empty(d, dtype=_FP32, device=x.device)
+    elif dgain is not None:
+        _full(dgain, "dgain", dev, (d,), _FP32)
+
+    def call(mem, nbytes):
+        return lib.ee_rms_norm_backward(dy.data_ptr(), _type(dy, "dy"), ld_dy, x.data_ptr(), _type(x, "x"), rows, d, ld_x,
+                                        gain.data_ptr(), _type(gain, "gain"), rstd.data_ptr(), _ptr(dx), ld_dx, _ptr(dgain),
+                                        mem, nbytes, _stream(dev))
+
+    rc = call(None, 0)
+    if rc == EE_ENOMEM:  # (a few rows need no scratch)
         nb = ctypes.c_size_t(0)
         check(lib.ee_rms_norm_scratch_bytes(rows, d, ctypes.byref(nb)))
-        nbytes = nb.value
-        mem = _scratch(nbytes, scratch, x) if nbytes else None
-    rc = lib.ee_rms_norm_backward(dy.data_ptr(), _type(dy, "dy"), ld_dy, x.data_ptr(), _type(x, "x"), rows, d, ld_x,
-                                  gain.data_ptr(), _type(gain, "gain"), rstd.data_ptr(), _ptr(dx), ld_dx, _ptr(dgain),
-                                  _ptr(mem), nbytes, _stream(dev))
+        rc = call(_scratch(nb.value, scratch, x).data_ptr(), nb.value)
     if rc != EE_OK:
         check(rc)
     return dx, dgain
