@@ -466,6 +466,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     volatile int* stall = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int w = __shfl_sync(kFull, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (threadIdx.x == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&ma) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&mb) : "memory");
         for (int i = 0; i < G::ST; ++i) {
             u_mb_init(&full[i], 1);
             u_mb_init(&empty[i], 1);
@@ -802,7 +804,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             }
             chain_read();
         }
-        if (tma && lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+        if (tma && lane == 0) tma_out_read<0>();  // (they finish with the grid)
     }
     __syncwarp();
     u_fence_before();

@@ -682,31 +682,29 @@ struct TopShared {
     unsigned long long best[kMaxList];
     unsigned long long surv[kEnough];
     uint16_t group[kMaxGroups * kNT];  // upper half of the order of each group's maximum
+    alignas(16) uint16_t mark[kNT];    // of each thread's
+    unsigned bound;
     unsigned hist[256];
     int list[kMaxHits];  // groups that may hold one of the best
     int join_n[kMaxCluster];
     int n_hits;
     int n;         // candidates pushed (may pass kCand: the surplus was dropped)
     int n_surv;
-    int2 sum[3];   // rotating counters of block_sum, zero between uses
+    int sum[3];    // rotating counters of block_sum, zero between uses
     unsigned long long prefix;
     int done;
     unsigned long long join[(kMaxCluster - 1) * kMaxList];  // the first CTA's, in clusters alone: the others' best
 };
 
-// Two sums over the consumers with one barrier: a slot is cleared two calls
-// before it is used again.
-__device__ __forceinline__ int2 block_sum(int a, int b, TopShared& sh, int& turn) {
-    a = __reduce_add_sync(kFull, a);
-    b = __reduce_add_sync(kFull, b);
+// Sum over the consumers with one barrier: a slot is cleared two calls before it is
+// used again.
+__device__ __forceinline__ int block_sum(int v, TopShared& sh, int& turn) {
+    v = __reduce_add_sync(kFull, v);
     const int slot = turn % 3;
-    if ((threadIdx.x & 31) == 0) {
-        if (a) atomicAdd(&sh.sum[slot].x, a);
-        if (b) atomicAdd(&sh.sum[slot].y, b);
-    }
+    if ((threadIdx.x & 31) == 0 && v) atomicAdd(&sh.sum[slot], v);
     consumers_sync<kNT>();
-    const int2 r = sh.sum[slot];
-    if (threadIdx.x == 0) sh.sum[(turn + 2) % 3] = make_int2(0, 0);
+    const int r = sh.sum[slot];
+    if (threadIdx.x == 0) sh.sum[(turn + 2) % 3] = 0;
     ++turn;
     return r;
 }
@@ -719,7 +717,7 @@ __device__ unsigned long long key_prefix(const unsigned long long* keys, int n, 
         const unsigned long long cand = P | 1ull << bit;
         int c = 0;
         for (int i = threadIdx.x; i < n; i += kNT) c += keys[i] >= cand;
-        c = block_sum(c, 0, sh, turn).x;
+        c = block_sum(c, sh, turn);
         if (c >= want) {
             P = cand;
             if (c <= kEnough) break;
@@ -819,20 +817,32 @@ __device__ __noinline__ int recollect(const Row<DT>& row, int v0, int v1, int k,
     return n;
 }
 
-// A bound that at least k of the threads' marks reach, and few more: four
-// candidates are counted per barrier, first in growing steps below the largest
-// value's order, then between the last that too few reached and the first that
-// enough did.
-__device__ unsigned mark_bound(int mark, int top, int k, TopShared& ts, int& turn) {
+// A bound that at least k of the threads' marks (ts.mark) reach, and few more, by
+// one warp: four candidates are counted per step, first in growing distances below
+// the largest value's order, then between the last that too few reached and the
+// first that enough did.  (With all warps and a barrier per step the selection's
+// instructions were a third more.)
+__device__ unsigned mark_bound(int top, int k, const TopShared& ts) {
     constexpr int kNone = 1 << 30;
+    const uint4 w = reinterpret_cast<const uint4*>(ts.mark)[threadIdx.x & 31];  // eight of them
+    static_assert(kNT == 8 * 32, "eight marks per lane");
+    const int mark[8] = {(int)(w.x & 0xffffu), (int)(w.x >> 16), (int)(w.y & 0xffffu), (int)(w.y >> 16),
+                         (int)(w.z & 0xffffu), (int)(w.z >> 16), (int)(w.w & 0xffffu), (int)(w.w >> 16)};
     const int few = k + k / 8 + 8;
     int lo = 1, hi = top + 1, at_lo = kNone;  // at_lo marks reach lo; too few reach hi
     for (int step = 4; at_lo > few && hi - lo > 1;) {
         int c[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) c[i] = at_lo == kNone ? max(lo, top - (step << (2 * i))) : lo + (hi - lo) * (4 - i) / 5;
-        const int2 s = block_sum((mark >= c[0]) + ((mark >= c[1]) << 16), (mark >= c[2]) + ((mark >= c[3]) << 16), ts, turn);
-        const int n[4] = {s.x & 0xffff, (int)((unsigned)s.x >> 16), s.y & 0xffff, (int)((unsigned)s.y >> 16)};
+        int n01 = 0, n23 = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            n01 += (mark[j] >= c[0]) + ((mark[j] >= c[1]) << 16);
+            n23 += (mark[j] >= c[2]) + ((mark[j] >= c[3]) << 16);
+        }
+        n01 = __reduce_add_sync(kFull, n01);
+        n23 = __reduce_add_sync(kFull, n23);
+        const int n[4] = {n01 & 0xffff, (int)((unsigned)n01 >> 16), n23 & 0xffff, (int)((unsigned)n23 >> 16)};
         int found = 4;
 #pragma unroll
         for (int i = 3; i >= 0; --i)
@@ -863,7 +873,12 @@ template <int DT>
 __device__ int slice_best(const Slice<DT, kNT>& s, int groups, int per, unsigned mark, float top, int k, TopShared& ts, int& turn) {
     constexpr int E = El<DT>::E;
     const int tid = threadIdx.x;
-    const unsigned P = mark_bound((int)mark, (int)(order_of(top) >> 16), k, ts, turn);
+    if (tid < 32) {  // (the marks are there since the row's reduction)
+        const unsigned b = mark_bound((int)(order_of(top) >> 16), k, ts);
+        if (tid == 0) ts.bound = b;
+    }
+    consumers_sync<kNT>();
+    const unsigned P = ts.bound;
     // the lowest value of that order; nothing but -inf lies below the first
     const float thr = P <= 0x7fu ? -FLT_MAX : value_of(P << 16);
     const unsigned least = max(P, order_of(-FLT_MAX) >> 16);
@@ -916,7 +931,7 @@ __global__ void __launch_bounds__(Geo<kNT>::threads, kCtas) k_logprobs(LogprobAr
     auto& l = *reinterpret_cast<Link<kNT>*>(l_smem + Geo<kNT>::ring);
     TopShared& ts = *reinterpret_cast<TopShared*>(l_smem + Geo<kNT>::ring + sizeof(Link<kNT>));
     const int rank = (int)(blockIdx.x % cs), tid = threadIdx.x, stride = gridDim.x / cs;
-    if (TOP && tid < 3) ts.sum[tid] = make_int2(0, 0);
+    if (TOP && tid < 3) ts.sum[tid] = 0;
     link_init(l, cs);
     Turn at;
     if (tid >= kNT) {
@@ -958,6 +973,7 @@ __global__ void __launch_bounds__(Geo<kNT>::threads, kCtas) k_logprobs(LogprobAr
             Run mine = acc.get();
             if (!ok) mine.s = kNan;
             const unsigned mark = order_of(top) >> 16;
+            if (TOP) ts.mark[tid] = (uint16_t)mark;
             const Run run = row_reduce<DT>(mine, l, c, i, rank, cs, TOP ? &top : nullptr);
             const bool none = run.m == -kInf && run.s == 0.f;
             const float lns = log_sum<DT>(run.s, run.m, c);
