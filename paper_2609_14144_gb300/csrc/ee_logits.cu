@@ -566,11 +566,11 @@ __device__ __forceinline__ void release(Link<NT>& l, const Turn& t) {
 }
 
 // One pass over the slice: many(cur, vb) takes this thread's vectors of a chunk
-// that lies wholly in the slice, vector vb + thread + u NT being cur[u];
-// one(w, v, vb) takes vector v of another chunk (-inf past the slice's end, called
+// that lies wholly in the slice, vector vb + thread + u NT being cur[u], or (QUADS)
+// the vectors vb + 4 thread .. + 3 in some order; one(w, v, vb) takes vector v of another chunk (-inf past the slice's end, called
 // by warps with any vector in it); after(n) follows the n-th chunk.  False once a
 // wait ran out.
-template <int DT, int NT, class Many, class One, class After>
+template <bool QUADS, int DT, int NT, class Many, class One, class After>
 __device__ __forceinline__ bool consume(const Slice<DT, NT>& s, const uint4* ring, Link<NT>& l, Turn& t, Many many, One one,
                                         After after) {
     bool ok = true;
@@ -581,16 +581,18 @@ __device__ __forceinline__ bool consume(const Slice<DT, NT>& s, const uint4* rin
         if (s.inner(vb)) {
             uint4 cur[kPer];
 #pragma unroll
-            for (int u = 0; u < kPer; ++u) cur[u] = st[u * NT];
+            for (int u = 0; u < kPer; ++u)
+                // (in quads the lanes' order is turned so that no two of eight share a bank)
+                cur[u] = QUADS ? st[3 * threadIdx.x + (u + threadIdx.x / 2) % 4] : st[u * NT];
             release(l, t);
             many(cur, vb);
         } else {
             const int end = min(s.f1, s.v1), warp = threadIdx.x & ~31;
 #pragma unroll 1
-            for (int u = 0; u < kPer && vb + warp + u * NT < s.v1; ++u) {
-                const int v = vb + threadIdx.x + u * NT;
+            for (int u = 0; u < kPer && vb + (QUADS ? 4 * warp + u : warp + u * NT) < s.v1; ++u) {
+                const int o = QUADS ? 3 * threadIdx.x + u : u * NT, v = vb + threadIdx.x + o;
                 uint4 w[1] = {make_uint4(El<DT>::ninf, El<DT>::ninf, El<DT>::ninf, El<DT>::ninf)};
-                if (v >= s.f0 && v < end) w[0] = st[u * NT];
+                if (v >= s.f0 && v < end) w[0] = st[o];
                 else if (v < s.v1) w[0] = s.row.load_edge((int64_t)v * El<DT>::E - s.row.mis);
                 one(w, v, vb);
             }
@@ -684,7 +686,7 @@ struct TopShared {
     uint16_t group[kMaxGroups * kNT];  // upper half of the order of each group's maximum
     alignas(16) uint16_t mark[kNT];    // of each thread's
     unsigned bound;
-    unsigned hist[256];
+    alignas(16) unsigned hist[kNT];
     int list[kMaxHits];  // groups that may hold one of the best
     int join_n[kMaxCluster];
     int n_hits;
@@ -817,11 +819,10 @@ __device__ __noinline__ int recollect(const Row<DT>& row, int v0, int v1, int k,
     return n;
 }
 
-// A bound that at least k of the threads' marks (ts.mark) reach, and few more, by
-// one warp: four candidates are counted per step, first in growing distances below
+// A bound that at least k of the threads' marks (ts.mark) reach, and few more, where
+// they spread too far for a histogram; by one warp: four candidates are counted per step, first in growing distances below
 // the largest value's order, then between the last that too few reached and the
-// first that enough did.  (With all warps and a barrier per step the selection's
-// instructions were a third more.)
+// first that enough did.
 __device__ unsigned mark_bound(int top, int k, const TopShared& ts) {
     constexpr int kNone = 1 << 30;
     const uint4 w = reinterpret_cast<const uint4*>(ts.mark)[threadIdx.x & 31];  // eight of them
@@ -867,43 +868,81 @@ __device__ unsigned mark_bound(int top, int k, const TopShared& ts) {
 // threads' marks reach bounds the k-th best element from below, and nearly as
 // tightly as the k-th best itself, as the best rarely share a thread.  Only the
 // groups of vectors whose maxima (ts.group) reach it, k and a few, are read
-// again, from L2.  Group j of thread t: its vectors of chunks [j per, (j + 1)
-// per).  Returns how many are in ts.best.
+// again.  Group j of thread t: its vectors of chunks [j per, (j + 1) per), four
+// neighbours in each, so that the second read takes whole sectors.  Returns how
+// many are in ts.best.
 template <int DT>
 __device__ int slice_best(const Slice<DT, kNT>& s, int groups, int per, unsigned mark, float top, int k, TopShared& ts, int& turn) {
     constexpr int E = El<DT>::E;
     const int tid = threadIdx.x;
-    if (tid < 32) {  // (the marks are there since the row's reduction)
-        const unsigned b = mark_bound((int)(order_of(top) >> 16), k, ts);
-        if (tid == 0) ts.bound = b;
+    // how far the marks lie below the largest value (bins of ts.hist, cleared at the
+    // row's start; NaN lies above it), and the nearest distance that holds k of them
+    const int top_mark = (int)(order_of(top) >> 16);
+    atomicAdd(&ts.hist[min(max(top_mark - (int)mark, 0), kNT - 1)], 1u);
+    consumers_sync<kNT>();
+    if (tid < 32) {
+        const uint4 a = reinterpret_cast<const uint4*>(ts.hist)[2 * tid], b = reinterpret_cast<const uint4*>(ts.hist)[2 * tid + 1];
+        const unsigned bin[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        unsigned sum = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += bin[j];
+        unsigned upto = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned v = __shfl_up_sync(kFull, upto, o);
+            if (tid >= o) upto += v;
+        }
+        const unsigned reach = __ballot_sync(kFull, upto >= (unsigned)k);
+        const int at = reach ? __ffs(reach) - 1 : 31;
+        unsigned far = 0, n = upto - sum;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (n < (unsigned)k) n += bin[j], far = 8 * tid + j;
+        far = __shfl_sync(kFull, far, at);
+        // (the last bin holds all that lies further)
+        const unsigned b0 = reach && far < kNT - 1 ? (unsigned)max(top_mark - (int)far, 1) : mark_bound(top_mark, k, ts);
+        if (tid == 0) ts.bound = b0;
     }
     consumers_sync<kNT>();
     const unsigned P = ts.bound;
     // the lowest value of that order; nothing but -inf lies below the first
     const float thr = P <= 0x7fu ? -FLT_MAX : value_of(P << 16);
     const unsigned least = max(P, order_of(-FLT_MAX) >> 16);
-    if (mark >= least)
-        for (int j = 0; j < groups; ++j)
-            if (ts.group[j * kNT + tid] >= least) {
-                const int at = atomicAdd(&ts.n_hits, 1);
-                if (at < kMaxHits) ts.list[at] = j * kNT + tid;
-            }
+    if (mark >= least) {
+        unsigned hit = 0;
+#pragma unroll
+        for (int j = 0; j < kMaxGroups; ++j)
+            if (j < groups && ts.group[j * kNT + tid] >= least) hit |= 1u << j;
+        int at = atomicAdd(&ts.n_hits, __popc(hit));
+        for (; hit; hit &= hit - 1, ++at)
+            if (at < kMaxHits) ts.list[at] = (__ffs(hit) - 1) * kNT + tid;
+    }
     consumers_sync<kNT>();
     const int hits = ts.n_hits;
     int n = kCand + 1;
     if (hits <= kMaxHits) {
-        const int vecs = per * kPer;  // of a group
-        for (int i = tid; i < hits * vecs; i += kNT) {
-            const int id = ts.list[i / vecs], q = i % vecs;
-            const int64_t v = s.v0 + ((int64_t)(id / kNT) * per * kPer + q) * kNT + id % kNT;
-            if (v >= s.v1) continue;
-            const uint4 w = s.row.load((int)v);
-            if (El<DT>::vmax(w) < thr) continue;
-            float x[E];
-            El<DT>::unpack(w, x);
+        for (int i = tid; i < hits * per; i += kNT) {
+            const int id = ts.list[i / per];
+            const int v = s.v0 + (id / kNT * per + i % per) * Geo<kNT>::chunk + id % kNT * kPer;
+            uint4 w[kPer];
+            if (v >= s.f0 && v + kPer <= min(s.f1, s.v1)) {  // (all four on their way at once)
+                const uint4* p = reinterpret_cast<const uint4*>(s.row.p + ((int64_t)v * E - s.row.mis));
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (!(x[e] < thr)) push(x[e], (int)(v * E - s.row.mis + e), ts);
+                for (int q = 0; q < kPer; ++q) w[q] = __ldg(p + q);
+            } else {
+#pragma unroll
+                for (int q = 0; q < kPer; ++q) w[q] = s.row.load_if(v + q, s.v1);
+            }
+            if (max_of<DT>(w) < thr) continue;
+#pragma unroll
+            for (int q = 0; q < kPer; ++q) {
+                if (El<DT>::vmax(w[q]) < thr) continue;
+                float x[E];
+                El<DT>::unpack(w[q], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (!(x[e] < thr)) push(x[e], (int)((int64_t)(v + q) * E - s.row.mis + e), ts);
+            }
         }
         consumers_sync<kNT>();
         n = ts.n;
@@ -950,8 +989,11 @@ __global__ void __launch_bounds__(Geo<kNT>::threads, kCtas) k_logprobs(LogprobAr
             Acc<DT, true> acc;
             int group = 0;
             float gm = -kInf, top = -kInf;  // largest of the group, of this thread's vectors
-            if (TOP && tid == 0) ts.n = ts.n_hits = 0;
-            const bool ok = consume(
+            if (TOP) {
+                ts.hist[tid] = 0;
+                if (tid == 0) ts.n = ts.n_hits = 0;
+            }
+            const bool ok = consume<true>(
                 s, ring, l, at,
                 [&](uint4(&cur)[kPer], int) {
                     const float vm = max_of<DT>(cur);
@@ -1370,7 +1412,7 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
                 const uint32_t m = bits[e >> 5] >> (e & 31) & ((1u << E) - 1);
                 if (m) w = El<DT>::without(w, m);
             };
-            ok &= consume(
+            ok &= consume<false>(
                 s, ring, l, at,
                 [&](uint4(&cur)[kPer], int vb) {
                     const uint32_t here = flags[(vb - s.v0) / Geo<kDNT>::chunk * Geo<kDNT>::warps + (tid >> 5)];  // (alike for the warp)
@@ -1404,7 +1446,7 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
                     for (int v = s.v0 + tid; v < s.v1; v += kDNT) out.put(s.row, v, make_uint4(0, 0, 0, 0));
                 } else {
                     const GradOf<DT> grad(coef, c, f);
-                    ok &= consume(
+                    ok &= consume<false>(
                         s, ring, l, at,
                         [&](uint4(&cur)[kPer], int vb) {
                             if (out.aligned) {
