@@ -1642,7 +1642,8 @@ int ee_distill_topk(const void* logits, int type, int64_t rows, int vocab, int64
     if ((uintptr_t)stats % 16) return fail(EE_EINVAL, "stats must be 16-byte aligned");
     int n_sm = 0;
     if ((rc = sm_count(&n_sm)) != EE_OK) return rc;
-    const int cs = cluster_size(rows, vocab, type, n_sm, kDCtas, Geo<kDNT>::chunk, grad != nullptr);
+    // (the same with and without the gradient, and so is the loss, bit for bit)
+    const int cs = cluster_size(rows, vocab, type, n_sm, kDCtas, Geo<kDNT>::chunk, true);
     const DistillArgs a{logits, ld, rows, vocab, k, tail ? 1 : 0, ids, ld_ids, teacher, ld_teacher, temperature, weight, loss,
                         reinterpret_cast<float4*>(stats), grad, ld_grad};
     cudaStream_t s = (cudaStream_t)stream;

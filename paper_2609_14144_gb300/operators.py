@@ -292,6 +292,7 @@ def token_logprobs(logits, ids=None, k: int = 0, temperature: float = 1.0, strea
     rows, vocab = logits.shape
     if ids is not None:
         _vec(ids, "ids", dev, rows, _INT32)
+    k = int(k)
     n = k if k > 0 else 0
     device = logits.device
     ent = torch.empty(rows, dtype=_FP32, device=device)

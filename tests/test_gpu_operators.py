@@ -197,6 +197,14 @@ def test_linear_long_rows_do_not_drift():
     assert ((y.double() - ref).abs() / ref).max().item() <= 2e-6
 
 
+@pytest.mark.parametrize("rows,n_in,n_out,out_dtype", [(1000, 30000, 500, BF16), (520, 20011, 300, FP32), (2100, 1536, 4000, FP32), (4100, 64, 2056, FP16)])
+def test_linear_wide_ranges_and_many_tiles(rows, n_in, n_out, out_dtype):
+    """Splits of k whose partial sums pass through memory, several tiles per CTA, every
+    type of result written by copies, with bias and residual."""
+    dtype = FP16 if out_dtype == FP16 else BF16
+    test_linear(rows, n_in, n_out, dtype, None, True, True, out_dtype, 8, 0)
+
+
 def test_linear_nan_and_inf_stay_in_their_rows():
     g = gen(4)
     x, w = normal(g, 140, 80, BF16), normal(g, 70, 80, BF16)
@@ -455,6 +463,27 @@ def test_distill(rows, V, k, dtype, T, pad, shift, tail):
     w = torch.rand(rows, generator=g, device="cuda") + 0.5
     w[2::5] = 0.0
     check_distill(z, ids, t, T, tail, w, in_place=pad == 0 and shift == 0)
+
+
+@pytest.mark.parametrize("dtype,pad", [(BF16, 0), (FP32, 0), (FP16, 3)])
+def test_distill_rows_shared_by_clusters(dtype, pad):
+    """More rows than clusters, each row a cluster's: lists and exchanges in turn."""
+    g = gen(31)
+    z = normal(g, 330, 100003, dtype, 3.0, pad)
+    ids, t = teacher_list(g, z, 5, 1.0, True)
+    w = torch.rand(330, generator=g, device="cuda") + 0.5
+    w[7::11] = 0.0
+    check_distill(z, ids, t, 1.0, True, w, in_place=pad == 0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+def test_distill_masks_of_the_lowest_value(dtype):
+    g = gen(32)
+    z = normal(g, 9, 3001, dtype, 2.0)
+    z[:, ::3] = torch.finfo(dtype).min
+    ids, t = teacher_list(g, z, 6, 1.0, True)
+    check_distill(z, ids, t, 1.0, True, torch.ones(9, device="cuda"))
+    check_distill(z, ids, t, 1.0, False, torch.ones(9, device="cuda"))
 
 
 @pytest.mark.parametrize("tail", [False, True])
