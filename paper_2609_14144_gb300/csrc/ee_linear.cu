@@ -419,10 +419,11 @@ __device__ __forceinline__ void sums32(uint32_t taddr, bool ok, float (&v)[32]) 
     }
 }
 
+constexpr int kChain = 8;  // stages the tensor core adds up by itself
+
 struct GemmArgs {
     int M, N, nk;        // nk: stages over the whole k range
     int mt, nt, S;       // tiles, k splits
-    int chain;           // stages the tensor core adds up by itself
     bool bf16, vec;
     bool tma;            // results (or partial sums) leave by TMA
     bool cluster;        // the splits of a tile are a cluster, which joins them
@@ -438,10 +439,9 @@ struct GemmArgs {
 // sums in registers, rounding to nearest: the tensor core truncates as it adds,
 // so a long range in one chain would drift (the error grows with its steps).
 // The next chain, or the next item's first, runs while one is read back.
-// Reading a chain back slows the MMAs beside it by about 600 cycles (measured
-// with chains of 8 stages, 640 cycles each): results of 32 bits take chains of 8
-// (k = 512), results of 16 bits chains of 32, whose drift of at most 128 * 2^-23
-// is far below their rounding.
+// Chains of 8 stages (k = 512), 32 steps of the tensor core, cost next to nothing
+// beside longer ones: forward and dx of 1024 x 1536 x 151936 take 609 us, with
+// chains of 16 and 32 stages 611 and 606.
 // The splits of a narrow tile may be the CTAs of a cluster (one item each): they
 // leave their sums in shared memory and each joins and writes a share of the rows,
 // without another launch.
@@ -565,14 +565,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             for (int it = first; it < items && ok; it += stride) {
                 const int s = it / tiles;
                 const int ks = (int)((int64_t)g.nk * (s + 1) / g.S) - (int)((int64_t)g.nk * s / g.S);
-                for (int c0 = 0; c0 < ks && ok; c0 += g.chain, ++u) {
+                for (int c0 = 0; c0 < ks && ok; c0 += kChain, ++u) {
                     if (u >= 2 && !__all_sync(kFull, u_mb_wait(&acc_empty[u & 1], ((u >> 1) - 1) & 1, stall))) {
                         *stall = kErrStall;
                         ok = false;
                         break;
                     }
                     u_fence_after();
-                    const int c1 = c0 + g.chain < ks ? c0 + g.chain : ks;
+                    const int c1 = c0 + kChain < ks ? c0 + kChain : ks;
                     for (int k = c0; k < c1; ++k) {
                         if (!__all_sync(kFull, u_mb_wait(&full[st], ph, stall))) {
                             *stall = kErrStall;
@@ -653,13 +653,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             };
             // The item's sums end up in the accumulator of its last chain, from where
             // they are written a few columns at a time.
-            if (ks <= g.chain) {
+            if (ks <= kChain) {
                 chain_full();
             } else {
                 float acc[HC];
 #pragma unroll
                 for (int i = 0; i < HC; ++i) acc[i] = 0.f;
-                for (int c0 = 0; c0 < ks; c0 += g.chain) {
+                for (int c0 = 0; c0 < ks; c0 += kChain) {
                     chain_full();
                     const uint32_t t = t0 + (u & 1) * BN;
 #pragma unroll
@@ -674,7 +674,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                             acc[c + 16 + i] += __uint_as_float(v1[i]);
                         }
                     }
-                    if (c0 + g.chain < ks) chain_read();
+                    if (c0 + kChain < ks) chain_read();
                 }
 #pragma unroll
                 for (int c = 0; c < HC; c += 16) {
@@ -1156,7 +1156,6 @@ int gemm(Ctx& c, Mat A, Mat B, const Epilogue& e) {
     g.N = (int)N;
     g.nk = (int)((K + kTK - 1) / kTK);
     g.bf16 = c.type == EE_BF16;
-    g.chain = e.out_type == EE_FP32 ? 8 : 32;
     g.vec = e.vec_all();
     const Tiling t = tiling(M, N, g.nk, c.n_sm);
     const int tm = t.pair ? 2 * kTM : kTM;
