@@ -436,7 +436,7 @@ __device__ __forceinline__ void consumers_sync() {
 
 template <int NT>
 struct Link {
-    uint64_t full[kStages], empty[kStages], list_ids[2], list_full[2], list_empty[2], exchange, joined;
+    uint64_t full[kStages], empty[kStages], list_ids[2], list_full[2], list_empty[2], reduced[2], exchange[2], joined;
     float4 peer[2][kMaxCluster];
     float4 warp[2][Geo<NT>::warps];
     int stall;  // a wait ran out: no further wait, results from here on are NaN
@@ -481,6 +481,26 @@ __device__ __forceinline__ void arrive_at(uint64_t* bar, int rank) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(p) : "memory");
 }
 
+// A state to another CTA's shared memory; its barrier counts the bytes.  (No fence:
+// one would wait for the thread's stores of the gradient, 8000 cycles a row.)
+__device__ __forceinline__ void send(float4* to, uint64_t* bar, int rank, const Run& r) {
+    uint32_t p, b;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(p) : "r"(u_saddr(to)), "r"(rank));
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(u_saddr(bar)), "r"(rank));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(p), "f"(r.m), "f"(r.s),
+                 "f"(r.a), "f"(0.f), "r"(b)
+                 : "memory");
+}
+// Nobody's shared memory is written after it left.
+template <int NT>
+__device__ __forceinline__ void leave(const Link<NT>& l, int cs) {
+    __syncwarp();
+    if (cs == 1) return;
+    cg::this_cluster().sync();
+    if (l.stall)  // a state that did not arrive in time may be on its way still: about 1 ms
+        for (const long long t0 = clock64(); clock64() - t0 < 2000000;) {}
+}
+
 template <int NT>
 __device__ void link_init(Link<NT>& l, int cs) {
     if (threadIdx.x == 0) {
@@ -491,9 +511,10 @@ __device__ void link_init(Link<NT>& l, int cs) {
         for (int i = 0; i < 2; ++i) {
             u_mb_init(&l.list_ids[i], 1);
             u_mb_init(&l.list_full[i], 1);
+            u_mb_init(&l.reduced[i], 1);
+            u_mb_init(&l.exchange[i], 1);
             u_mb_init(&l.list_empty[i], Geo<NT>::warps);
         }
-        u_mb_init(&l.exchange, cs);
         u_mb_init(&l.joined, cs > 1 ? cs - 1 : 1);
         l.stall = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -645,11 +666,10 @@ __device__ __forceinline__ Run row_reduce(Run r, Link<NT>& l, float c, int turn,
         for (int i = 0; i < Geo<NT>::warps; ++i) *top = fmaxf(*top, l.warp[p][i].w);
     if (cs > 1) {
         if (threadIdx.x < cs) {
-            cg::cluster_group cl = cg::this_cluster();
-            *cl.map_shared_rank(&l.peer[p][rank], threadIdx.x) = make_float4(r.m, r.s, r.a, 0.f);
-            arrive_at(&l.exchange, threadIdx.x);
+            if (threadIdx.x == 0) expect_tx(&l.exchange[p], 16 * cs);
+            send(&l.peer[p][rank], &l.exchange[p], threadIdx.x, r);
         }
-        const bool ok = wait(l, &l.exchange, p);
+        const bool ok = wait(l, &l.exchange[p], turn >> 1 & 1);
         r = join_states<DT>(l.peer[p], cs, c);
         if (!ok) r.s = kNan;
     }
@@ -1084,8 +1104,7 @@ __global__ void __launch_bounds__(Geo<kNT>::threads, kCtas) k_logprobs(LogprobAr
             }
         }
     }
-    __syncwarp();
-    if (cs > 1) cg::this_cluster().sync();  // nobody's shared memory is written after it left
+    leave(l, cs);
 }
 
 // ---------------------------------------------------------------- distillation
@@ -1116,22 +1135,19 @@ struct DistillArgs {
 
 // What a row's list gives by itself.
 struct ListShared {
-    double q[kMaxList], c;  // weights; sum of q (log q - x / T)
-    double sum, inv_t;      // sum of q
+    double c, sum;          // sums of q (log q - x / T) and of q
     alignas(16) int id[kMaxList];  // -1: absent
     float x[kMaxList];      // the row's value there
     float t[kMaxList];      // the teacher's value
+    float q[kMaxList];      // weight
     float merged[kMaxList]; // weight of the token, all its entries together
     int next[kMaxList];     // -1: absent or named by an earlier entry; else how many later ones name it
     float q0, m, s;         // what the list leaves over; largest x, sum of powers relative to it
+    Run o;                  // the unlisted elements' softmax, for the loss
 };
+constexpr int kSeen = 512;  // words of the filter that finds tokens listed twice
 
 __device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
-    return v;
-}
-__device__ __forceinline__ double warp_sum(double v) {
 #pragma unroll
     for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
     return v;
@@ -1158,11 +1174,10 @@ __device__ __forceinline__ void list_read(const DistillArgs& a, const Row<DT>& r
 }
 
 // Whether no earlier entry names entry i's token; ls.next[i].
-__device__ __forceinline__ bool list_first(int k, int i, ListShared& ls) {
+__device__ __noinline__ bool list_first(int k, int i, ListShared& ls) {
     const int id = ls.id[i];
     int before = 0, after = 0;  // other entries of the same token
     const int4* all = reinterpret_cast<const int4*>(ls.id);
-#pragma unroll 4
     for (int j = 0; j < k; j += 4) {
         const int4 o = all[j >> 2];
         before += (j < i && o.x == id) + (j + 1 < i && o.y == id) + (j + 2 < i && o.z == id) + (j + 3 < i && o.w == id);
@@ -1172,28 +1187,75 @@ __device__ __forceinline__ bool list_first(int k, int i, ListShared& ls) {
     ls.next[i] = first ? after : -1;
     return first;
 }
+// ls.next for every entry, and how many tokens are listed (one warp).  Lists seldom
+// name a token twice: each sets a bit of a filter (seen, left clear), and only where
+// two share one are the entries compared with one another.
+__device__ __forceinline__ int list_marks(int k, ListShared& ls, uint32_t* seen) {
+    const int lane = threadIdx.x & 31;
+    bool twice = false;
+    for (int i = lane; i < k; i += 32) {
+        const uint32_t h = (uint32_t)ls.id[i] * 2654435769u >> 18;
+        if (ls.id[i] >= 0) twice |= atomicOr(&seen[h >> 5], 1u << (h & 31)) >> (h & 31) & 1;
+    }
+    twice = __any_sync(kFull, twice);
+    __syncwarp();
+    int listed = 0;
+    for (int i = lane; i < k; i += 32) {
+        const uint32_t h = (uint32_t)ls.id[i] * 2654435769u >> 18;
+        if (ls.id[i] >= 0) seen[h >> 5] = 0;
+        if (twice) {
+            listed += list_first(k, i, ls);
+        } else {
+            ls.next[i] = ls.id[i] >= 0 ? 0 : -1;
+            listed += ls.id[i] >= 0;
+        }
+    }
+    __syncwarp();
+    return __reduce_add_sync(kFull, listed);
+}
 // ls.merged: what the gradient needs of the weights, q of each token (one warp).
-template <class Q>
-__device__ __forceinline__ void list_merge(int k, ListShared& ls, Q q) {
+__device__ __forceinline__ void list_merge(int k, ListShared& ls, float scale) {
     __syncwarp();
     for (int i = threadIdx.x & 31; i < k; i += 32) {
-        auto sum = q(i);
+        float sum = ls.q[i];
         if (ls.next[i] > 0)
             for (int j = i + 1; j < k; ++j)
-                if (ls.id[j] == ls.id[i]) sum += q(j);
-        ls.merged[i] = (float)sum;
+                if (ls.id[j] == ls.id[i]) sum += ls.q[j];
+        ls.merged[i] = sum * scale;
     }
 }
 
-// What follows from the list by itself (one warp).  The weights and the loss's
-// part are formed in 64 bits: the loss is a small difference of terms q log q and
-// q log p, and q0 one of 1 and sum q; this warp has the time of a row for it.
+// e^(d + dl), d in (-87, 88), as hi + lo, to about 2^-26: Cody and Waite's reduction by n ln 2 (ln 2 in
+// a part of 12 bits, whose products with n are exact, and the rest), then the
+// exponential series; the two leading terms are added without loss.
+struct Pair {
+    float hi, lo;
+};
+__device__ __forceinline__ Pair exp_pair(float d, float dl) {
+    const float n = rintf(d * 1.44269504f);
+    const float r = fmaf(n, -2839.f / 4096.f, d);              // exact
+    const float rl = fmaf(n, -3.1946184945e-5f, dl);          // ln 2 - 2839 / 4096
+    const float x = r + rl;
+    float p = 1.f / 40320.f;
+    p = fmaf(p, x, 1.f / 5040.f);
+    p = fmaf(p, x, 1.f / 720.f);
+    p = fmaf(p, x, 1.f / 120.f);
+    p = fmaf(p, x, 1.f / 24.f);
+    p = fmaf(p, x, 1.f / 6.f);
+    p = fmaf(p, x, 0.5f);
+    const float a = 1.f + r, b = r - (a - 1.f);                // 1 + r = a + b
+    const float lo = b + fmaf(p, x * x, rl), hi = a + lo;
+    return Pair{ldexpf(hi, (int)n), ldexpf(lo - (hi - a), (int)n)};
+}
+
+// What follows from the list by itself (one warp).  The loss is a small difference
+// of terms q log q and q log p, and q0 one of 1 and sum q: the weights in it
+// carry 26 bits and its sums 64.  (In 64 bits throughout, the list took longer than its row:
+// 18 us of the 13.6 that 4096 rows of 151936 bf16 have at the memory's rate.)
 template <int DT>
-__device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls, uint64_t* ids_known) {
+__device__ void list_prepare(const DistillArgs& a, float c, double inv_t, ListShared& ls, uint32_t* seen, uint64_t* ids_known) {
     const int lane = threadIdx.x & 31;
-    int listed = 0;
-    for (int i = lane; i < a.k; i += 32) listed += list_first(a.k, i, ls);
-    __syncwarp();
+    const int listed = list_marks(a.k, ls, seen);
     if (lane == 0) u_mb_arrive(ids_known);  // the row can be streamed meanwhile
     float tm = -kInf, m = -kInf;
     for (int i = lane; i < a.k; i += 32) {
@@ -1203,31 +1265,42 @@ __device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls, uint
     tm = warp_max_nan(tm);
     m = warp_max_nan(m);
     if (a.tail || tm == -kInf) tm = 0.f;
-    double z = 0.0;
+    double z = 0.0, part = 0.0;  // sums of e = e^(t - tm) and of e (t - x / T)
     float s = 0.f;
     for (int i = lane; i < a.k; i += 32) {
-        if (ls.next[i] >= 0) s += ex2(exponent<DT>(ls.x[i], m, c));
-        const double e = exp((double)ls.t[i] - tm);
-        ls.q[i] = e;
-        z += e;
+        const float t = ls.t[i], x = ls.x[i], d = t - tm, back = t - d;
+        if (ls.next[i] >= 0) s += ex2(exponent<DT>(x, m, c));
+        double ed;
+        if (d > -87.f && d < 88.f) {
+            const Pair e = exp_pair(d, (t - (d + back)) - (tm - back));
+            ed = (double)e.hi + e.lo;
+        } else {
+            ed = exp((double)t - tm);
+        }
+        ls.q[i] = (float)ed;
+        z += ed;
+        if (ed > 0.0 || ed != ed) part = fma(ed, t - x * inv_t, part);
     }
-    z = warp_sum(z);
-    s = warp_sum(s);
-    listed = __reduce_add_sync(kFull, listed);
-    const double inv_t = 1.0 / (double)a.temperature;
-    const double scale = a.tail || z == 0.0 ? 1.0 : 1.0 / z, shift = a.tail || z == 0.0 ? 0.0 : tm + log(z);
-    double part = 0.0;
-    for (int i = lane; i < a.k; i += 32) {
-        const double q = ls.q[i] * scale;
-        ls.q[i] = q;
-        if (q > 0.0 || q != q) part += q * (((double)ls.t[i] - shift) - ls.x[i] * inv_t);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        z += __shfl_xor_sync(kFull, z, o);
+        part += __shfl_xor_sync(kFull, part, o);
+        s += __shfl_xor_sync(kFull, s, o);
     }
-    part = warp_sum(part);
-    list_merge(a.k, ls, [&](int i) { return ls.q[i]; });
+    // renormalised: q = e / z, log q = t - tm - log z
+    const float zf = (float)z;
+    double scale = 1.0, shift = 0.0;
+    if (!a.tail && z != 0.0) {
+        scale = 1.f / zf;
+        scale *= 2.0 - z * scale;
+        const float y = logf(zf);  // and a Newton step
+        const Pair e = exp_pair(-y, 0.f);
+        shift = (double)tm + y + fma(z, (double)e.hi + e.lo, -1.0);
+    }
+    list_merge(a.k, ls, (float)scale);
     if (lane == 0) {
-        ls.c = part;
         ls.sum = z * scale;
-        ls.inv_t = inv_t;
+        ls.c = part * scale - (shift == 0.0 ? 0.0 : shift * ls.sum);
         ls.m = m;
         ls.s = s;
         double q0 = a.tail ? fmax(0.0, 1.0 - z) : 0.0;
@@ -1239,45 +1312,62 @@ __device__ void list_prepare(const DistillArgs& a, float c, ListShared& ls, uint
 
 // The weights alone, in 32 bits: all that the backward pass needs of the list
 // (one warp, in every CTA of a row; the 64-bit form took 21 of its 207 us).
-__device__ void list_weights(const DistillArgs& a, ListShared& ls) {
+__device__ void list_weights(const DistillArgs& a, ListShared& ls, uint32_t* seen) {
     const int lane = threadIdx.x & 31;
+    list_marks(a.k, ls, seen);
     float tm = -kInf, z = 0.f;
     for (int i = lane; i < a.k; i += 32) tm = fmaxf(tm, ls.t[i]);
     tm = warp_max_nan(tm);
     if (a.tail || tm == -kInf) tm = 0.f;
     for (int i = lane; i < a.k; i += 32) {
-        list_first(a.k, i, ls);
         const float e = expf(ls.t[i] - tm);
         ls.q[i] = e;
         z += e;
     }
     z = warp_sum(z);
-    const float scale = a.tail || z == 0.f ? 1.f : 1.f / z;
-    list_merge(a.k, ls, [&](int i) { return (float)ls.q[i] * scale; });
+    list_merge(a.k, ls, a.tail || z == 0.f ? 1.f : 1.f / z);
 }
 
-// Gradient coefficients (x: mo, y: alpha, z: M, w: Q / S) of a row from its list
-// and the unlisted elements' softmax; *loss where it is asked for.
+// A row's softmax from its list's and the unlisted elements'.
+struct RowSum {
+    float M, up, S, q0;  // reference, powers of the unlisted relative to it, sum, what the list leaves over
+};
 template <int DT>
-__device__ __forceinline__ float4 row_finish(const DistillArgs& a, const Run& o, float c, const ListShared& ls, float* loss) {
+__device__ __forceinline__ RowSum row_sum(const DistillArgs& a, const Run& o, float c, const ListShared& ls) {
+    RowSum r;
     // where the rest is masked out, what rounding leaves of 1 - sum q is nothing
-    const float q0 = o.s == 0.f && ls.q0 < (float)a.k * 0x1p-22f ? 0.f : ls.q0;
-    const float M = max_nan(o.m, ls.m);
-    const float up = o.m == -kInf ? 0.f : ex2_full(shift_of<DT>(o.m, M, c));  // the unlisted powers relative to M
-    const float ul = ls.m == -kInf ? 0.f : ex2_full(shift_of<DT>(ls.m, M, c));
-    const float S = fmaf(o.s, up, ls.s * ul), Q = (float)ls.sum;
-    const bool none = S == 0.f;  // no finite logit in the row
-    const float k = none ? 0.f : (Q + q0) / S;
-    if (loss) {
-        const double lse = none ? -kInf : M * ls.inv_t + (double)log_sum<DT>(S, M, c);
-        double v = none ? (Q > 0.f || q0 > 0.f ? (double)kInf : Q != Q ? (double)kNan : 0.0) : ls.c + ls.sum * lse;
-        if (!none && (q0 > 0.f || q0 != q0)) {
-            const double lse0 = o.s == 0.f ? -kInf : o.m * ls.inv_t + (double)log_sum<DT>(o.s, o.m, c);
-            v += q0 * ((double)logf(q0) - (lse0 - lse));
+    r.q0 = o.s == 0.f && ls.q0 < (float)a.k * 0x1p-22f ? 0.f : ls.q0;
+    r.M = max_nan(o.m, ls.m);
+    r.up = o.m == -kInf ? 0.f : ex2_full(shift_of<DT>(o.m, r.M, c));
+    const float ul = ls.m == -kInf ? 0.f : ex2_full(shift_of<DT>(ls.m, r.M, c));
+    r.S = fmaf(o.s, r.up, ls.s * ul);
+    return r;
+}
+// Gradient coefficients: x: mo, y: alpha, z: M, w: Q / S (0 for a row without a finite
+// logit).
+template <int DT>
+__device__ __forceinline__ float4 row_coef(const DistillArgs& a, const Run& o, float c, const ListShared& ls) {
+    const RowSum r = row_sum<DT>(a, o, c, ls);
+    const float k = r.S == 0.f ? 0.f : ((float)ls.sum + r.q0) / r.S;
+    return make_float4(o.m, o.s == 0.f ? 0.f : k * r.up - r.q0 / o.s, r.M, k);
+}
+// The loss, by the warp that prepares lists, beside the gradient's writing.
+template <int DT>
+__device__ float row_loss(const DistillArgs& a, const Run& o, float c, double inv_t, const ListShared& ls) {
+    const RowSum r = row_sum<DT>(a, o, c, ls);
+    const double Q = ls.sum;
+    double v;
+    if (r.S == 0.f) {
+        v = Q > 0.0 || r.q0 > 0.f ? (double)kInf : Q != Q ? (double)kNan : 0.0;
+    } else {
+        const double lse = r.M * inv_t + (double)log_sum<DT>(r.S, r.M, c);
+        v = ls.c + Q * lse;
+        if (r.q0 > 0.f || r.q0 != r.q0) {
+            const double lse0 = o.s == 0.f ? -kInf : o.m * inv_t + (double)log_sum<DT>(o.s, o.m, c);
+            v += r.q0 * ((double)logf(r.q0) - (lse0 - lse));
         }
-        *loss = (float)(v * a.temperature * a.temperature);
     }
-    return make_float4(o.m, o.s == 0.f ? 0.f : k * up - q0 / o.s, M, k);
+    return (float)(v * a.temperature * a.temperature);
 }
 
 // The gradient of an unlisted vector, alpha 2^((x - mo) c).
@@ -1360,11 +1450,12 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
     auto& l = *reinterpret_cast<Link<kDNT>*>(l_smem + Geo<kDNT>::ring);
     ListShared* lists = reinterpret_cast<ListShared*>(l_smem + Geo<kDNT>::ring + sizeof(Link<kDNT>));
     // which vectors of a warp's in a chunk hold listed elements; a bit per element
-    uint32_t* flags = reinterpret_cast<uint32_t*>(lists + 2);
+    uint32_t* seen = reinterpret_cast<uint32_t*>(lists + 2);
+    uint32_t* flags = seen + kSeen;
     uint32_t* bits = flags + slice_flags(a.vocab, E, cs);
     const int rank = (int)(blockIdx.x % cs), tid = threadIdx.x, stride = gridDim.x / cs;
     const float c = 1.4426950408889634f / a.temperature;
-    for (int i = tid; i < slice_flags(a.vocab, E, cs) + slice_words(a.vocab, E, cs); i += Geo<kDNT>::threads) flags[i] = 0;
+    for (int i = tid; i < kSeen + slice_flags(a.vocab, E, cs) + slice_words(a.vocab, E, cs); i += Geo<kDNT>::threads) seen[i] = 0;
     link_init(l, cs);
     if (tid >= kDNT) {
         if (tid == kDNT) {
@@ -1377,15 +1468,29 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
             }
             drain(l, at, n);
         } else if (tid >= kDNT + 32) {
+            const double inv_t = 1.0 / (double)a.temperature;
+            // the loss of row number i, once its sums are there
+            auto loss = [&](int64_t r, int i) {
+                if (rank) return;
+                const bool ok = wait(l, &l.reduced[i & 1], (i >> 1) & 1);
+                const float v = row_loss<DT>(a, lists[i & 1].o, c, inv_t, lists[i & 1]);
+                if (tid == kDNT + 32) a.loss[r] = ok ? v : kNan;
+            };
             int i = 0;
-            for (int64_t r = blockIdx.x / cs; r < a.rows; r += stride, ++i) {
-                bool ok = i < 2 || wait(l, &l.list_empty[i & 1], ((i >> 1) - 1) & 1);
-                if (!__all_sync(kFull, ok)) break;
+            bool ok = true;
+            int64_t r = blockIdx.x / cs;
+            for (; r < a.rows && ok; r += stride, ++i) {
+                ok = i < 2 || wait(l, &l.list_empty[i & 1], ((i >> 1) - 1) & 1);
+                if (!(ok = __all_sync(kFull, ok))) break;
                 list_read<DT>(a, Row<DT>(a.logits, a.ld, r, a.vocab), r, lists[i & 1], tid & 31, 32);
                 __syncwarp();
-                list_prepare<DT>(a, c, lists[i & 1], &l.list_ids[i & 1]);
+                list_prepare<DT>(a, c, inv_t, lists[i & 1], seen, &l.list_ids[i & 1]);
                 if (tid == kDNT + 32) u_mb_arrive(&l.list_full[i & 1]);
+                if (i) loss(r - stride, i - 1);
             }
+            if (i) loss(r - stride, i - 1);
+            if (!ok && rank == 0 && tid == kDNT + 32)  // a wait ran out
+                for (; r < a.rows; r += stride) a.loss[r] = kNan;
         }
     } else {
         Turn at;
@@ -1433,10 +1538,10 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
             if (!ok) run.s = kNan;
             run = row_reduce<DT>(run, l, c, i, rank, cs, nullptr);
             if (bit >= 0) bits[bit >> 5] = flags[flag] = 0;  // (all are past the row; the next one's are set after the barrier below)
-            float loss;
-            const float4 coef = row_finish<DT>(a, run, c, ls, rank == 0 && tid == 0 ? &loss : nullptr);
+            const float4 coef = row_coef<DT>(a, run, c, ls);
             if (rank == 0 && tid == 0) {
-                a.loss[r] = loss;
+                lists[i & 1].o = run;
+                u_mb_arrive(&l.reduced[i & 1]);
                 if (a.stats) a.stats[r] = coef;
             }
             if constexpr (GRAD) {
@@ -1474,8 +1579,7 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
             if ((tid & 31) == 0) u_mb_arrive(&l.list_empty[i & 1]);
         }
     }
-    __syncwarp();
-    if (cs > 1) cg::this_cluster().sync();  // nobody's shared memory is written after it left
+    leave(l, cs);
 }
 
 // The gradient alone, from the forward pass's statistics: a CTA per chunk of a
@@ -1483,6 +1587,7 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
 template <int DT>
 __global__ void __launch_bounds__(kBT) k_distill_backward(DistillArgs a, int chunks) {
     __shared__ ListShared ls;
+    __shared__ uint32_t seen[kSeen];
     const int64_t r = blockIdx.x / chunks;
     const int ch = (int)(blockIdx.x % chunks);
     const Row<DT> row(a.logits, a.ld, r, a.vocab);
@@ -1499,8 +1604,9 @@ __global__ void __launch_bounds__(kBT) k_distill_backward(DistillArgs a, int chu
 #pragma unroll
     for (int u = 0; u < kLU; ++u) nxt[u] = row.load_if(v0 + threadIdx.x + u * kBT, v1);
     list_read<DT>(a, row, r, ls, threadIdx.x, kBT);
+    for (int i = threadIdx.x; i < kSeen; i += kBT) seen[i] = 0;
     __syncthreads();  // the listed values are read before the row may be overwritten
-    if (threadIdx.x >= kBT - 32) list_weights(a, ls);
+    if (threadIdx.x >= kBT - 32) list_weights(a, ls, seen);
     for (int vb = v0; vb < v1; vb += kBT * kLU) {
         uint4 cur[kLU];
 #pragma unroll
@@ -1587,7 +1693,7 @@ int run_logprobs(const LogprobArgs& a, int cs, int n_sm, cudaStream_t s) {
 
 template <int DT>
 int run_distill(const DistillArgs& a, int cs, int n_sm, cudaStream_t s) {
-    const size_t smem = Geo<kDNT>::ring + sizeof(Link<kDNT>) + 2 * sizeof(ListShared) + 4 * (size_t)(slice_flags(a.vocab, El<DT>::E, cs) + slice_words(a.vocab, El<DT>::E, cs));
+    const size_t smem = Geo<kDNT>::ring + sizeof(Link<kDNT>) + 2 * sizeof(ListShared) + 4 * (size_t)(kSeen + slice_flags(a.vocab, El<DT>::E, cs) + slice_words(a.vocab, El<DT>::E, cs));
     return a.grad ? launch_rows(k_distill<DT, true>, a.rows, cs, kDCtas * n_sm, Geo<kDNT>::threads, smem, s, a)
                   : launch_rows(k_distill<DT, false>, a.rows, cs, kDCtas * n_sm, Geo<kDNT>::threads, smem, s, a);
 }
