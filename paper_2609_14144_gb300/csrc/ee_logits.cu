@@ -1250,8 +1250,8 @@ __device__ __forceinline__ Pair exp_pair(float d, float dl) {
 
 // What follows from the list by itself (one warp).  The loss is a small difference
 // of terms q log q and q log p, and q0 one of 1 and sum q: the weights in it
-// carry 26 bits and its sums 64.  (In 64 bits throughout, the list took longer than its row:
-// 18 us of the 13.6 that 4096 rows of 151936 bf16 have at the memory's rate.)
+// carry 26 bits and its sums 64.  (About 6500 cycles for 64 entries, in the shadow of
+// the 30000 that a row of 151936 bf16 takes.)
 template <int DT>
 __device__ void list_prepare(const DistillArgs& a, float c, double inv_t, ListShared& ls, uint32_t* seen, uint64_t* ids_known) {
     const int lane = threadIdx.x & 31;
