@@ -119,16 +119,34 @@ __device__ __forceinline__ void store8(void* p, int type, int n, bool vec, const
 __host__ __device__ __forceinline__ int bytes_of(int type) { return type == EE_FP32 ? 4 : 2; }
 
 // ---------------------------------------------------------------- activations
+// 1 / (1 + e^-u), from e^-|u|: the divisor lies in [1, 2], where the short division
+// is good to 2 ulp (with a full one 2048 x 1536 -> 8960 took 105 us, relu 48).
+__device__ __forceinline__ float sigmoid(float u) {
+    const float e = expf(-fabsf(u)), r = __fdividef(1.f, 1.f + e);
+    return u >= 0.f ? r : e * r;
+}
 __device__ __forceinline__ float act_value(float u, int act) {
     if (act == EE_ACT_RELU) return u > 0.f || u != u ? u : 0.f;
-    if (act == EE_ACT_SILU) return u / (1.f + expf(-u));
+    if (act == EE_ACT_SILU) return u * sigmoid(u);
     if (act == EE_ACT_GELU) return 0.5f * u * (1.f + erff(u * 0.70710678f));
     return u;
+}
+__device__ __forceinline__ void act8(float (&v)[8], int act) {  // (one branch for all)
+    if (act == EE_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = act_value(v[i], EE_ACT_RELU);
+    } else if (act == EE_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = act_value(v[i], EE_ACT_SILU);
+    } else if (act == EE_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = act_value(v[i], EE_ACT_GELU);
+    }
 }
 __device__ __forceinline__ float act_slope(float u, int act) {
     if (act == EE_ACT_RELU) return u > 0.f ? 1.f : 0.f;
     if (act == EE_ACT_SILU) {
-        const float g = 1.f / (1.f + expf(-u));
+        const float g = sigmoid(u);
         return g * fmaf(u, 1.f - g, 1.f);
     }
     if (act == EE_ACT_GELU) return 0.5f * (1.f + erff(u * 0.70710678f)) + u * expf(-0.5f * u * u) * 0.39894228f;
@@ -149,6 +167,7 @@ struct Epilogue {
         return vec_out && (!bias || vec_bias) && (!res || vec_res) && (!preact || vec_pre);
     }
 };
+template <bool ACT = true>
 __device__ __forceinline__ void emit8(const Epilogue& e, int64_t row, int64_t col, int n, float (&v)[8]) {
     if (e.bias) {
         float b[8];
@@ -157,10 +176,7 @@ __device__ __forceinline__ void emit8(const Epilogue& e, int64_t row, int64_t co
         for (int i = 0; i < 8; ++i) v[i] += b[i];
     }
     if (e.preact) store8(e.preact + row * e.ld_pre + col, EE_FP32, n, e.vec_pre, v);
-    if (e.act != EE_ACT_NONE) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = act_value(v[i], e.act);
-    }
+    if (ACT) act8(v, e.act);
     if (e.res) {
         float r[8];
         load8((const char*)e.res + (row * e.ld_res + col) * bytes_of(e.out_type), e.out_type, n, e.vec_res, r);
@@ -170,7 +186,50 @@ __device__ __forceinline__ void emit8(const Epilogue& e, int64_t row, int64_t co
     store8((char*)e.out + (row * e.ld_out + col) * bytes_of(e.out_type), e.out_type, n, e.vec_out, v);
 }
 
-// The same without an activation for four rows, row0 + 8 i, of a block whose
+// Eight elements a stride of `step` bytes apart.
+__device__ __forceinline__ void load_column(const char* p, int64_t step, int type, float (&x)[8]) {
+    if (type == EE_FP32) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k, p += step) x[k] = *(const float*)p;
+    } else {
+        uint16_t h[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k, p += step) h[k] = *(const uint16_t*)p;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = get16(h[k], type);
+    }
+}
+__device__ __forceinline__ void store_column(char* p, int64_t step, int type, const float (&x)[8]) {
+    if (type == EE_FP32) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k, p += step) *(float*)p = x[k];
+    } else {
+        uint32_t w[4];
+        pack8(x, type, w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k, p += step) *(uint16_t*)p = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+    }
+}
+// Bias to rounding for eight rows of one column: for results off the 16-byte grid,
+// where a warp's 32 lanes write neighbouring columns and each step is done for the
+// eight together (1024 x 1536 -> 50257 bf16: 124 us; by pieces of 8 columns 291).
+template <bool ACT>
+__device__ __forceinline__ void emit_column(const Epilogue& e, int64_t row0, int64_t col, float bias, float (&v)[8]) {
+    const int es = bytes_of(e.out_type);
+    float r[8] = {};
+    if (e.res) load_column((const char*)e.res + (row0 * e.ld_res + col) * es, e.ld_res * es, e.out_type, r);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += bias;
+    if (e.preact) store_column((char*)(e.preact + row0 * e.ld_pre + col), e.ld_pre * 4, EE_FP32, v);
+    if (ACT) act8(v, e.act);
+    if (e.res) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += r[k];
+    }
+    store_column((char*)e.out + (row0 * e.ld_out + col) * es, e.ld_out * es, e.out_type, v);
+}
+
+// emit8 without an activation for four rows, row0 + 8 i, of a block whose
 // 16-byte accesses are all in range and aligned: each step is done for the four
 // together, so that their accesses are in flight at the same time.
 __device__ __forceinline__ void emit8x4(const Epilogue& e, int64_t row0, int64_t col, float (&v)[4][8]) {
@@ -420,6 +479,18 @@ __device__ __forceinline__ void sums32(uint32_t taddr, bool ok, float (&v)[32]) 
     }
 }
 
+// 8 columns.
+__device__ __forceinline__ void sums8(uint32_t taddr, bool ok, float (&v)[8]) {
+    uint32_t a[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(a[4]), "=r"(a[5]), "=r"(a[6]), "=r"(a[7])
+                 : "r"(taddr)
+                 : "memory");
+    u_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = ok ? __uint_as_float(a[i]) : kNan;
+}
+
 constexpr int kChain = 8;  // stages the tensor core adds up by itself
 
 struct GemmArgs {
@@ -446,9 +517,12 @@ struct GemmArgs {
 // The splits of a narrow tile may be the CTAs of a cluster (one item each): they
 // leave their sums in shared memory and each joins and writes a share of the rows,
 // without another launch.
+// ACT: results pass through an activation (a kernel of its own: its code slowed the
+// others by 3%).  They leave by TMA too: 2048 x 1536 -> 8960 takes 48, 58 and 64 us
+// for relu, silu and gelu.
 // A wait that runs out (about 2 s) ends the CTA's loops; its remaining items
 // are written as NaN.
-template <int BN, bool PAIR, bool A_MN, bool B_MN>
+template <int BN, bool PAIR, bool A_MN, bool B_MN, bool ACT>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     k_gemm(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
            const __grid_constant__ CUtensorMap mo, const __grid_constant__ CUtensorMap mr, GemmArgs g) {
@@ -708,6 +782,41 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                         ok = __all_sync(kFull, ok);
                         res_ph ^= 1 << (c & 1);
                     }
+                    if (ACT && g.S == 1) {  // 8 columns at a time: the code is long
+#pragma unroll 1
+                        for (int j = 0; j < cw / 8; ++j) {
+                            float v[8];
+                            sums8(sums + c * cw + 8 * j, ok, v);
+                            if (bias) {
+                                float b = bias_of[0];
+#pragma unroll
+                                for (int p = 1; p < HC / 32; ++p) b = (c * cw + 8 * j) / 32 == p ? bias_of[p] : b;
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) v[i] += __shfl_sync(kFull, b, (8 * j & 31) + i);
+                            }
+                            act8(v, g.e.act);
+                            if (f32) {
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    float4* p = reinterpret_cast<float4*>(blk + (((2 * j + i) ^ swz) << 4));
+                                    float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+                                    if (res) r = *p;
+                                    *p = make_float4(v[4 * i] + r.x, v[4 * i + 1] + r.y, v[4 * i + 2] + r.z, v[4 * i + 3] + r.w);
+                                }
+                            } else {
+                                uint4* p = reinterpret_cast<uint4*>(blk + ((j ^ swz) << 4));
+                                if (res) {
+                                    float x[8];
+                                    unpack8(*p, g.e.type, x);
+#pragma unroll
+                                    for (int i = 0; i < 8; ++i) v[i] += x[i];
+                                }
+                                uint32_t o[4];
+                                pack8(v, g.e.type, o);
+                                *p = make_uint4(o[0], o[1], o[2], o[3]);
+                            }
+                        }
+                    } else
 #pragma unroll 1
                     for (int half = 0; half < (f32 ? 1 : 2); ++half) {
                         float v[32];
@@ -777,6 +886,22 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                 for (int j = 0; j < 8; ++j)
                     s4[lane * 8 + (j ^ (lane & 7))] = make_float4(x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]);
                 __syncwarp();
+                if (g.S == 1 && !g.vec && m0 + 32 <= g.M) {
+                    const int col = n0 + c + lane;
+                    if (col < g.N) {
+                        const float b = g.e.bias ? get16(((const uint16_t*)g.e.bias)[col], g.e.type) : 0.f;
+#pragma unroll 1
+                        for (int r = 0; r < 32; r += 8) {
+                            float v[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                v[k] = reinterpret_cast<const float*>(so)[(r + k) * 32 + ((lane >> 2 ^ k) << 2) + (lane & 3)];
+                            emit_column<ACT>(g.e, m0 + r, col, b, v);
+                        }
+                    }
+                    __syncwarp();
+                    continue;
+                }
                 const int col = n0 + c + 8 * (lane & 3), ch = 2 * (lane & 3), row = m0 + (lane >> 2);
                 auto piece = [&](int i, float (&v)[8]) {
                     const int lr = 8 * i + (lane >> 2);
@@ -784,7 +909,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                     v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
                     v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
                 };
-                if (g.S == 1 && g.e.act == EE_ACT_NONE && g.vec && m0 + 32 <= g.M && n0 + c + 32 <= g.N) {
+                if ((!ACT || g.e.act == EE_ACT_NONE) && g.S == 1 && g.vec && m0 + 32 <= g.M && n0 + c + 32 <= g.N) {
                     float v[4][8];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) piece(i, v[i]);
@@ -798,7 +923,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                         if (g.S > 1)
                             store8(g.part + ((int64_t)s * g.M + row + 8 * i) * g.ldp + col, EE_FP32, 8, true, v);
                         else
-                            emit8(g.e, row + 8 * i, col, g.N - col, v);
+                            emit8<ACT>(g.e, row + 8 * i, col, g.N - col, v);
                     }
                 }
                 __syncwarp();
@@ -832,7 +957,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                         // (a copy that outlasted its wait may have landed on a stalled split's NaN)
                         if (*cl.map_shared_rank(const_cast<int*>(stall), k)) v[0] = v[1] = v[2] = v[3] = v[4] = v[5] = v[6] = v[7] = kNan;
                     }
-                    emit8(g.e, row, col, g.N - col, v);
+                    emit8<ACT>(g.e, row, col, g.N - col, v);
                 }
             }
             __syncwarp();
@@ -1136,14 +1261,14 @@ bool make_out_map(CUtensorMap* map, const void* p, int64_t N, int64_t M, int64_t
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BN, bool PAIR, bool A_MN, bool B_MN>
+template <int BN, bool PAIR, bool A_MN, bool B_MN, bool ACT>
 int launch_gemm(const Ctx& c, const Mat& A, const Mat& B, GemmArgs g) {
     using G = GShape<BN, PAIR>;
     CUtensorMap ma, mb, mo{}, mr{};
-    // results leave by TMA where their rows allow it and nothing has to be computed
-    // between the sums and the residual
+    // results leave by TMA where their rows allow it and no value before the activation
+    // is kept
     const Epilogue& e2 = g.e;
-    g.tma = G::blocks && (g.S > 1 || (e2.act == EE_ACT_NONE && !e2.preact && e2.vec_out && (!e2.res || e2.vec_res)));
+    g.tma = G::blocks && (g.S > 1 || (!e2.preact && e2.vec_out && (!e2.res || e2.vec_res)));
     if (g.tma) {
         const bool ok = g.S > 1 ? make_out_map(&mo, g.part, g.ldp, g.M, g.S, g.ldp, EE_FP32, 3)
                                 : make_out_map(&mo, e2.out, g.N, g.M, 1, e2.ld_out, e2.out_type, 3) &&
@@ -1152,7 +1277,7 @@ int launch_gemm(const Ctx& c, const Mat& A, const Mat& B, GemmArgs g) {
     }
     if (!make_map(&ma, A, c.type, A_MN ? kTK : kTM) || !make_map(&mb, B, c.type, B_MN ? kTK : G::b_rows))
         return fail(EE_ECUDA, "cuTensorMapEncodeTiled failed");
-    auto* k = k_gemm<BN, PAIR, A_MN, B_MN>;
+    auto* k = k_gemm<BN, PAIR, A_MN, B_MN, ACT>;
     cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)G::smem);
     if (e != cudaSuccess) return cuda_status(e);
     cudaLaunchConfig_t cfg{};
@@ -1186,6 +1311,15 @@ int launch_gemm(const Ctx& c, const Mat& A, const Mat& B, GemmArgs g) {
     return cuda_status(cudaLaunchKernelEx(&cfg, k, ma, mb, mo, mr, g));
 }
 
+template <bool A_MN, bool B_MN, bool ACT>
+int launch_tiles(const Ctx& c, const Mat& A, const Mat& B, const GemmArgs& g, const Tiling& t) {
+    if (t.pair)
+        return t.bn == 256 ? launch_gemm<256, true, A_MN, B_MN, ACT>(c, A, B, g) : launch_gemm<128, true, A_MN, B_MN, ACT>(c, A, B, g);
+    return t.bn == 256   ? launch_gemm<256, false, A_MN, B_MN, ACT>(c, A, B, g)
+           : t.bn == 128 ? launch_gemm<128, false, A_MN, B_MN, ACT>(c, A, B, g)
+                         : launch_gemm<64, false, A_MN, B_MN, ACT>(c, A, B, g);
+}
+
 // D = A B^T.  A_MN / B_MN: the operand is stored with k as its rows.
 template <bool A_MN, bool B_MN>
 int gemm(Ctx& c, const Mat& A, const Mat& B, const Epilogue& e) {
@@ -1209,12 +1343,9 @@ int gemm(Ctx& c, const Mat& A, const Mat& B, const Epilogue& e) {
     if (t.S > 1 && !t.cluster) g.part = (float*)c.mem.take(4 * (size_t)t.S * M * g.ldp);
     g.e = e;
     if (c.dry) return EE_OK;
-    if (t.pair)
-        rc = t.bn == 256 ? launch_gemm<256, true, A_MN, B_MN>(c, A, B, g) : launch_gemm<128, true, A_MN, B_MN>(c, A, B, g);
-    else
-        rc = t.bn == 256   ? launch_gemm<256, false, A_MN, B_MN>(c, A, B, g)
-             : t.bn == 128 ? launch_gemm<128, false, A_MN, B_MN>(c, A, B, g)
-                           : launch_gemm<64, false, A_MN, B_MN>(c, A, B, g);
+    // (partial sums have no activation; only results do, and those are the forward pass's)
+    const bool act = e.act != EE_ACT_NONE && (t.S == 1 || t.cluster);
+    rc = act ? launch_tiles<A_MN, B_MN, !A_MN && !B_MN>(c, A, B, g, t) : launch_tiles<A_MN, B_MN, false>(c, A, B, g, t);
     if (rc != EE_OK || t.S == 1 || t.cluster) return rc;
     return launch_ahead(k_join, (unsigned)n_blocks(M * (g.ldp / 8), 256), c.s, g);
 }

@@ -205,6 +205,27 @@ def test_linear_wide_ranges_and_many_tiles(rows, n_in, n_out, out_dtype):
     test_linear(rows, n_in, n_out, dtype, None, True, True, out_dtype, 8, 0)
 
 
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+@pytest.mark.parametrize("n_out,dtype,out_dtype,pad", [(4000, BF16, BF16, 8), (4000, FP16, FP32, 3), (4001, FP16, FP16, 0), (4001, BF16, FP32, 0)])
+def test_linear_activations_of_wide_tiles(act, n_out, dtype, out_dtype, pad):
+    """Behind wide tiles results leave by copies, by 16-byte pieces (with the value before
+    the activation) or, off the 16-byte grid, column by column."""
+    test_linear(2090, 192, n_out, dtype, act, True, True, out_dtype, pad, 0)
+
+
+@pytest.mark.parametrize("rows", [1, 8, 200])
+def test_linear_silu_over_its_range(rows):
+    """The quotient a few units (16 of 2^-24), and e^-|u| a step of the subnormals at most,
+    times |u| < 2^7; outside of that zero or u, and NaN where u e^-|u| is."""
+    u = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 0.5, -0.5, 17.0, -17.0, 60.0, -60.0, 87.0, -87.0, 88.5, -88.5, 100.0, -100.0, 127.0, -127.0, 300.0, -300.0,
+                      3e38, -3e38, math.inf, -math.inf, math.nan], device="cuda").to(BF16)
+    x = torch.zeros((rows, 1), dtype=BF16, device="cuda") + 1
+    y = ee.linear(x, u[:, None].contiguous(), activation="silu", out_dtype=FP32).double()
+    U = u.double()
+    ref = (U * torch.sigmoid(U)).expand(rows, -1)
+    within(y, ref, 16 * 2.0 ** -24 * ref.abs() + 2.0 ** -142, "silu")
+
+
 def test_linear_nan_and_inf_stay_in_their_rows():
     g = gen(4)
     x, w = normal(g, 140, 80, BF16), normal(g, 70, 80, BF16)
