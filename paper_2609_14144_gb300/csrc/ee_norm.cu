@@ -40,13 +40,20 @@ __device__ __forceinline__ int bytes_of(int type) { return type == EE_FP32 ? 4 :
 struct Raw {
     uint4 a, b;  // b: fp32 alone
 };
-// Columns [8 j, 8 j + 8) of a row of d; columns past d read as 0.  VEC: all rows
-// lie on 16-byte boundaries and d is a multiple of 8, so that nothing but the
-// thread's place decides and the loads of several rows go out together.
+// Column e of the eight of chunk j.  VEC: all rows lie on 16-byte boundaries and d is
+// a multiple of 8, so that chunks are 16-byte accesses of which nothing but the
+// thread's place decides and the loads of several rows go out together.  Otherwise
+// a warp's lanes take neighbouring columns (8192 x 2047 bf16 with chunks of
+// neighbours: 58 us forward, 77 backward, now 40 and 59; aligned 2048: 19 and 31).
+template <bool VEC>
+__device__ __forceinline__ int column(int j, int e) {
+    return VEC ? 8 * j + e : ((j & ~31) << 3) + 32 * e + (j & 31);
+}
+// Chunk j of a row of d; columns past d read as 0.
 template <bool VEC>
 __device__ __forceinline__ Raw load_raw(const void* row, int type, int j, int d) {
     Raw r{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-    const int c = 8 * j;
+    const int c = column<VEC>(j, 0);
     if (VEC) {
         if (c < d) {
             const uint4* p = (const uint4*)((const char*)row + (int64_t)c * bytes_of(type));
@@ -60,14 +67,14 @@ __device__ __forceinline__ Raw load_raw(const void* row, int type, int j, int d)
         uint32_t* w = &r.a.x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (c + i < d) w[i] = p[i];
-            if (c + 4 + i < d) (&r.b.x)[i] = p[4 + i];
+            if (c + 32 * i < d) w[i] = p[32 * i];
+            if (c + 128 + 32 * i < d) (&r.b.x)[i] = p[128 + 32 * i];
         }
     } else {
         const uint16_t* p = (const uint16_t*)row + c;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (c + i < d) (&r.a.x)[i / 2] |= (uint32_t)p[i] << (16 * (i & 1));
+            if (c + 32 * i < d) (&r.a.x)[i / 2] |= (uint32_t)p[32 * i] << (16 * (i & 1));
     }
     return r;
 }
@@ -95,7 +102,7 @@ __device__ __forceinline__ void to_float(const Raw& r, int type, float (&x)[8]) 
 }
 template <bool VEC>
 __device__ __forceinline__ void store8(void* row, int type, int j, int d, const float (&x)[8]) {
-    const int c = 8 * j;
+    const int c = column<VEC>(j, 0);
     char* p = (char*)row + (int64_t)c * bytes_of(type);
     if (type == EE_FP32) {
         if (VEC) {
@@ -105,7 +112,7 @@ __device__ __forceinline__ void store8(void* row, int type, int j, int d, const 
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (c + i < d) ((float*)p)[i] = x[i];
+                if (c + 32 * i < d) ((float*)p)[32 * i] = x[i];
         }
         return;
     }
@@ -125,7 +132,7 @@ __device__ __forceinline__ void store8(void* row, int type, int j, int d, const 
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            if (c + i < d) ((uint16_t*)p)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+            if (c + 32 * i < d) ((uint16_t*)p)[32 * i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
     }
 }
 
@@ -271,7 +278,7 @@ __global__ void __launch_bounds__(CPT == 1 ? 256 : kNormThreads, CPT == 1 ? 3 : 
     if (part)
 #pragma unroll
         for (int i = 0; i < CPT; ++i)
-            store8<false>(part + (int64_t)blockIdx.x * d, EE_FP32, threadIdx.x + i * blockDim.x, d, dg[i]);
+            store8<VEC>(part + (int64_t)blockIdx.x * d, EE_FP32, threadIdx.x + i * blockDim.x, d, dg[i]);
 }
 
 // ---------------------------------------------------------------- ring of rows
@@ -488,7 +495,7 @@ __global__ void __launch_bounds__(kNormThreads, 1)
     for (int i = 0; i < CPT; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int c = 8 * (threadIdx.x + i * blockDim.x) + e;
+            const int c = column<VEC>(threadIdx.x + i * blockDim.x, e);
             if (c < d) few_dg[c] = dg[i][e];
         }
     cg::cluster_group cl = cg::this_cluster();
