@@ -1426,6 +1426,45 @@ struct GradRow {
         for (int e = 0; e < E; ++e)
             if (b + e >= 0 && b + e < row.V) g[b + e] = o[e];
     }
+    // The same by a whole warp, whose lanes have neighbouring vectors that lie wholly in
+    // the row, where the gradient's rows start elsewhere in their 16 bytes than the
+    // logits': a lane joins the end of its vector with the start of the next lane's.
+    // (1024 x 50256 bf16, rows 3 further apart in the logits, step 99 us, backward pass 54; by elements 176 and 160.)
+    __device__ __forceinline__ void put_shifted(const Row<DT>& row, int v, const uint4& out) const {
+        constexpr int E = El<DT>::E;
+        T* p = g + ((int64_t)v * E - row.mis);
+        const int s = (int)((uintptr_t)p & 15), lane = threadIdx.x & 31, q = (16 - s) >> 2;  // (s > 0, the same for the warp)
+        uint32_t a[9] = {out.x, out.y, out.z, out.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[4 + i] = __shfl_down_sync(kFull, a[i], 1);
+        a[8] = 0;
+        // the 16 bytes from byte 16 - s on
+#pragma unroll
+        for (int i = 0; i < 7; ++i) a[i] = q & 2 ? a[i + 2] : a[i];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) a[i] = q & 1 ? a[i + 1] : a[i];
+        const int r = 8 * (s & 3 ? 4 - (s & 3) : 0);
+        if (lane < 31)
+            __stcs(reinterpret_cast<uint4*>((char*)p - s + 16),
+                   make_uint4(__funnelshift_r(a[0], a[1], r), __funnelshift_r(a[1], a[2], r), __funnelshift_r(a[2], a[3], r),
+                              __funnelshift_r(a[3], a[4], r)));
+        if (lane == 0 || lane == 31) {  // the warp's first and last bytes
+            const T* o = reinterpret_cast<const T*>(&out);
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if ((e * (int)sizeof(T) < 16 - s) == (lane == 0)) p[e] = o[e];
+        }
+    }
+    // Zeros for vectors [v0, v1).
+    __device__ void zero(const Row<DT>& row, int v0, int v1, int threads) const {
+        constexpr int E = El<DT>::E;
+        if (aligned) {
+            for (int v = v0 + threadIdx.x; v < v1; v += threads) put(row, v, make_uint4(0, 0, 0, 0));
+            return;
+        }
+        const int64_t e1 = min((int64_t)v1 * E - row.mis, (int64_t)row.V);
+        for (int64_t e = max((int64_t)v0 * E - row.mis, (int64_t)0) + threadIdx.x; e < e1; e += threads) g[e] = El<DT>::put(0.f);
+    }
     // The listed elements of vectors [v0, v1), over what put() left there.  (A row
     // without a finite logit has no softmax: no gradient.)
     __device__ void listed(const DistillArgs& a, const Row<DT>& row, int v0, int v1, float c, float f, float4 coef,
@@ -1548,7 +1587,7 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
                 const float w = a.weight ? a.weight[r] : 1.f, f = w * a.temperature;
                 const GradRow<DT> out(a, s.row, r);
                 if (w == 0.f) {  // rows outside the batch: zeros, whatever they hold
-                    for (int v = s.v0 + tid; v < s.v1; v += kDNT) out.put(s.row, v, make_uint4(0, 0, 0, 0));
+                    out.zero(s.row, s.v0, s.v1, kDNT);
                 } else {
                     const GradOf<DT> grad(coef, c, f);
                     ok &= consume<false>(
@@ -1560,7 +1599,7 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
                                 for (int u = 0; u < kPer; ++u) __stcs(to + u * kDNT, grad(cur[u]));
                             } else {
 #pragma unroll
-                                for (int u = 0; u < kPer; ++u) out.put(s.row, vb + tid + u * kDNT, grad(cur[u]));
+                                for (int u = 0; u < kPer; ++u) out.put_shifted(s.row, vb + tid + u * kDNT, grad(cur[u]));
                             }
                         },
                         [&](uint4(&x)[1], int v, int) {
@@ -1586,6 +1625,7 @@ __global__ void __launch_bounds__(Geo<kDNT>::threads, kDCtas) k_distill(DistillA
 // row, four vectors per thread in flight.
 template <int DT>
 __global__ void __launch_bounds__(kBT) k_distill_backward(DistillArgs a, int chunks) {
+    constexpr int E = El<DT>::E;
     __shared__ ListShared ls;
     __shared__ uint32_t seen[kSeen];
     const int64_t r = blockIdx.x / chunks;
@@ -1595,7 +1635,7 @@ __global__ void __launch_bounds__(kBT) k_distill_backward(DistillArgs a, int chu
     const float c = 1.4426950408889634f / a.temperature, w = a.weight[r], f = w * a.temperature;
     const GradRow<DT> out(a, row, r);
     if (w == 0.f) {
-        for (int v = v0 + threadIdx.x; v < v1; v += kBT) out.put(row, v, make_uint4(0, 0, 0, 0));
+        out.zero(row, v0, v1, kBT);
         return;
     }
     const float4 coef = a.stats[r];
@@ -1616,8 +1656,11 @@ __global__ void __launch_bounds__(kBT) k_distill_backward(DistillArgs a, int chu
         }
 #pragma unroll
         for (int u = 0; u < kLU; ++u) {
-            const int v = vb + threadIdx.x + u * kBT;
-            if (v < v1) out.put(row, v, grad(cur[u]));
+            const int v = vb + threadIdx.x + u * kBT, w0 = v - (threadIdx.x & 31);
+            if (!out.aligned && w0 + 32 <= v1 && w0 >= (row.mis ? 1 : 0) && (int64_t)(w0 + 32) * E - row.mis <= row.V)
+                out.put_shifted(row, v, grad(cur[u]));
+            else if (v < v1)
+                out.put(row, v, grad(cur[u]));
         }
     }
     __syncthreads();

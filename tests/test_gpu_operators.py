@@ -498,6 +498,32 @@ def test_distill_rows_shared_by_clusters(dtype, pad):
 
 
 @pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
+@pytest.mark.parametrize("V", [257, 12288, 40003])
+def test_distill_gradient_rows_on_any_boundary(dtype, V):
+    """The gradient's bits do not depend on where its rows start in their 16 bytes, and
+    nothing around them is written."""
+    g = gen(V)
+    rows, k = 4, 5
+    ids = torch.randint(0, V, (rows, k), generator=g, device="cuda", dtype=torch.int32)
+    t = torch.randn((rows, k), generator=g, device="cuda")
+    w = torch.tensor([1.0, 0.0, -0.5, 2.0], device="cuda")
+    for z in (normal(g, rows, V, dtype, 2.0, 0, 0), normal(g, rows, V, dtype, 2.0, 5, 3)):
+        _, stats = ee.distill_topk(z, ids, t)
+        ways = [lambda out: ee.distill_topk_step(z, ids, t, w, grad=out)[1],
+                lambda out: ee.distill_topk_backward(w, z, ids, t, stats, grad=out)]
+        wants = [way(None) for way in ways]
+        for shift in range(16 // z.element_size()):
+            for pad in (0, 1, 5):
+                for way, want in zip(ways, wants):
+                    out = normal(g, rows, V, dtype, 1.0, pad, shift)
+                    assert way(out) is out
+                    assert torch.equal(out, want), (shift, pad)
+                    after = out.as_strided((rows - 1, pad), (V + pad, 1), shift + V)
+                    before = out.as_strided((shift,), (1,), 0)
+                    assert torch.isnan(after).all() and torch.isnan(before).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP16, FP32])
 def test_distill_masks_of_the_lowest_value(dtype):
     g = gen(32)
     z = normal(g, 9, 3001, dtype, 2.0)
