@@ -1248,6 +1248,14 @@ __device__ __forceinline__ Pair exp_pair(float d, float dl) {
     return Pair{ldexpf(hi, (int)n), ldexpf(lo - (hi - a), (int)n)};
 }
 
+// ln z to about 2^-26: a Newton step on logf's.
+__device__ __forceinline__ double log_fine(double z) {
+    const float y = logf((float)z);
+    if (!(y > -87.f && y < 87.f)) return y;  // (infinities, NaN and what nears them)
+    const Pair e = exp_pair(-y, 0.f);
+    return y + fma(z, (double)e.hi + e.lo, -1.0);
+}
+
 // What follows from the list by itself (one warp).  The loss is a small difference
 // of terms q log q and q log p, and q0 one of 1 and sum q: the weights in it
 // carry 26 bits and its sums 64.  (About 6500 cycles for 64 entries, in the shadow of
@@ -1293,9 +1301,7 @@ __device__ void list_prepare(const DistillArgs& a, float c, double inv_t, ListSh
     if (!a.tail && z != 0.0) {
         scale = 1.f / zf;
         scale *= 2.0 - z * scale;
-        const float y = logf(zf);  // and a Newton step
-        const Pair e = exp_pair(-y, 0.f);
-        shift = (double)tm + y + fma(z, (double)e.hi + e.lo, -1.0);
+        shift = tm + log_fine(z);
     }
     list_merge(a.k, ls, (float)scale);
     if (lane == 0) {
@@ -1351,6 +1357,13 @@ __device__ __forceinline__ float4 row_coef(const DistillArgs& a, const Run& o, f
     const float k = r.S == 0.f ? 0.f : ((float)ls.sum + r.q0) / r.S;
     return make_float4(o.m, o.s == 0.f ? 0.f : k * r.up - r.q0 / o.s, r.M, k);
 }
+// log_sum, for the loss: where student and teacher are alike it is a small difference
+// of logarithms, and their roundings to 32 bits would be seen in it.
+template <int DT>
+__device__ __forceinline__ double log_sum_fine(float s, float m, float c) {
+    const double lns = log_fine(s);
+    return m == -kInf || wide<DT>(m, c) ? lns : lns - fmaf(m, c, -ref_of(m, c)) * 0.6931471805599453;
+}
 // The loss, by the warp that prepares lists, beside the gradient's writing.
 template <int DT>
 __device__ float row_loss(const DistillArgs& a, const Run& o, float c, double inv_t, const ListShared& ls) {
@@ -1360,11 +1373,11 @@ __device__ float row_loss(const DistillArgs& a, const Run& o, float c, double in
     if (r.S == 0.f) {
         v = Q > 0.0 || r.q0 > 0.f ? (double)kInf : Q != Q ? (double)kNan : 0.0;
     } else {
-        const double lse = r.M * inv_t + (double)log_sum<DT>(r.S, r.M, c);
+        const double lse = r.M * inv_t + log_sum_fine<DT>(r.S, r.M, c);
         v = ls.c + Q * lse;
         if (r.q0 > 0.f || r.q0 != r.q0) {
-            const double lse0 = o.s == 0.f ? -kInf : o.m * inv_t + (double)log_sum<DT>(o.s, o.m, c);
-            v += r.q0 * ((double)logf(r.q0) - (lse0 - lse));
+            const double lse0 = o.s == 0.f ? -kInf : o.m * inv_t + log_sum_fine<DT>(o.s, o.m, c);
+            v += r.q0 * (log_fine(r.q0) - (lse0 - lse));
         }
     }
     return (float)(v * a.temperature * a.temperature);
