@@ -411,7 +411,8 @@ constexpr int kStages = 3;
 // NT consuming threads.  The log probabilities take 256 and three CTAs per SM, so
 // that one selects while two stream (145 us for 2048 rows of 151936 with 64 best;
 // 157 with two CTAs of 384); the distillation's rows in flight have to fit in L2,
-// and it takes 384 and two (486 us for 4096 rows; 508 with 256, 521 with three CTAs).
+// and it takes 384 and two (428 us for 4096 rows; before the exchange between CTAs was
+// made short 486, 508 with 256 threads, 521 with three CTAs).
 template <int NT>
 struct Geo {
     static constexpr int warps = NT / 32, threads = NT + 64;
@@ -1317,7 +1318,7 @@ __device__ void list_prepare(const DistillArgs& a, float c, double inv_t, ListSh
 }
 
 // The weights alone, in 32 bits: all that the backward pass needs of the list
-// (one warp, in every CTA of a row; the 64-bit form took 21 of its 207 us).
+// (one warp, in every CTA of a row; in 64 bits they took 21 of its 207 us).
 __device__ void list_weights(const DistillArgs& a, ListShared& ls, uint32_t* seen) {
     const int lane = threadIdx.x & 31;
     list_marks(a.k, ls, seen);
